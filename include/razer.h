@@ -255,6 +255,77 @@ int razer_gemm_w4a4_fp4(const razer_desc* d, const void* packed_w_dev, const voi
                         const float* act_tensor_scale_dev, int M, void* y_dev, void* workspace_dev,
                         size_t workspace_bytes, void* stream);
 
+/* ---- Eight bits, for what four do not serve: layers kept in 8-bit integers, and the cache of keys and values (App. C.1
+ * quantizes the cache beside weights and activations).  All calls here are asynchronous on `stream` and are launched with
+ * programmatic dependent launch, but touch nothing that the kernel ahead of them may own before it has finished: their operands
+ * may come from any kernel directly ahead.  A scale is FP32 and not negative, value = scale * code. */
+
+/* Rows to 8-bit integers: scales_dev[m] = fl32(max_k |x[m][k]| / 127), codes_dev[m][k] = the exact quotient x / scale to the
+ * nearest integer, ties to even, at most 127 in magnitude (-128 is never written).  A row of zeros has scale 0; the quotient of
+ * a row that is not, if it rounds to 0, becomes 2^-149; a row with a NaN or an infinity has scale NaN and codes 0.
+ * x_dev: bf16, or FP32 where x_is_fp32 != 0, [M][K] with row_stride elements from one row to the next (>= K), K a multiple of
+ * 16, 16-byte aligned rows.  Tokens online (M tokens) and weights offline (one scale for each output channel, M = N). */
+int razer_quant_i8(const void* x_dev, int x_is_fp32, int M, int K, long long row_stride, int8_t* codes_dev,
+                   float* scales_dev, void* stream);
+
+/* Matrix product of 8-bit integers with a scale for each token and channel:
+ * y[m][n] = bf16( fl32(x_scales[m] * w_scales[n]) * sum_k x_codes[m][k] * w_codes[n][k] ), the sum exact in 32 bits, any M >= 1
+ * and N >= 1.  x_codes_dev int8 [M][K], w_codes_dev int8 [N][K] (16-byte aligned, any codes, -128 included), K a multiple of 16 up to
+ * 131056; y_dev bf16 [M][N].  Weights are taken as razer_quant_i8 writes them: no layout step and no workspace.  If a
+ * device-side wait gives up (razer_workspace_status), the outputs concerned are NaN. */
+int razer_gemm_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev,
+                  const float* w_scales_dev, int M, int N, int K, void* y_dev, void* stream);
+
+/* One layer's cache of keys and values in 8-bit integers, in pages of tokens with a scale for each page and head. */
+typedef struct razer_kv8 {
+  int32_t pages;        /* pages in the pools, >= 1; pages * heads < 2^31                     */
+  int32_t page;         /* tokens of a page: 16, 32, 64 or 128                              */
+  int32_t heads;        /* key-value heads, 1 .. 32767                                      */
+  int32_t head_dim;     /* 64 or 128                                                        */
+  int8_t* k_codes_dev;  /* [pages][heads][page][head_dim], 16-byte aligned                  */
+  int8_t* v_codes_dev;
+  float* k_scales_dev;  /* [pages][heads]                                                   */
+  float* v_scales_dev;
+} razer_kv8;
+
+/* What both calls below take of a batch of B sequences (device arrays, read on the device: lengths never come to the host):
+ *   block_table_dev int32 [B][table_width]  token p of sequence b is in row p % page of page block_table[b][p / page]
+ *   q_start_dev     int32 [B + 1]           sequence b's new tokens are rows q_start[b] .. q_start[b + 1] - 1, not decreasing
+ *   kv_len_dev      int32 [B]               tokens of sequence b, the new ones included: they are its last ones
+ *   T                                       rows that the buffers have; rows from q_start[B] on (a padded batch) are left alone
+ * table_width * page must be below 2^31 - 1024.  Entries of the table behind a sequence's last page are not looked at.  A sequence
+ * whose rows do not lie in 0 .. T - 1 counts as having none; B = 0 or T = 0 is a call without work.
+ *
+ * razer_kv8_append: writes the new tokens' keys and values, bf16 [T][heads][head_dim], k_stride and v_stride elements from one token
+ * to the next (multiples of 8, so that columns of a wider matrix serve; 16-byte aligned).  For each page and head that gets
+ * tokens, with s0 the scale so far (0 where the page's first token is new) and a the largest new magnitude: the scale becomes
+ * s = max(s0, fl32(a / 127)) (2^-149 as in razer_quant_i8); where s > s0 > 0 the page's older codes become the nearest integers to
+ * the exact code * s0 / s; the new codes are the nearest integers to the exact x / s.  A NaN or an infinity among the new values, or s0 NaN,
+ * makes the page's scale NaN for that head (new codes 0, older codes as they were).  Codes behind the last token are left as they were.  Tokens whose
+ * page the table does not name (an entry outside 0 .. pages - 1, or behind table_width) or whose position is negative (more new
+ * tokens than kv_len) are not written.  A page that gets tokens belongs to one sequence; pages that sequences share must be full
+ * ones. */
+int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_stride, const void* v_new_dev,
+                     long long v_stride, const int32_t* block_table_dev, int table_width,
+                     const int32_t* q_start_dev, const int32_t* kv_len_dev, int B, int T, void* stream);
+
+/* Causal attention of the new tokens' queries over the cache that already holds them (razer_kv8_append first).  q_dev: bf16
+ * [T][q_heads][head_dim], q_stride elements from one token to the next (a multiple of 8, 16-byte aligned); q_heads a multiple of
+ * the cache's heads, query head i reads key-value head i / (q_heads / heads).  The row of a token at position p = kv_len - n + i sees
+ * the keys 0 .. p:
+ *   s_j = scale * k_scale(page of j) * <q, k_code_j>,  out = sum_j exp(s_j) v_scale(page of j) v_code_j / sum_j exp(s_j)
+ * out_dev: bf16 [T][q_heads][head_dim], 16-byte aligned; lse_dev: FP32 [T][q_heads], log sum_j exp(s_j), or NULL.  A row that
+ * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN shows as NaN in the rows that see its page, and so does
+ * a page that the table does not name; a sequence longer than the table gets NaN in all its rows.  Sums are FP32; query
+ * rows and probabilities are rounded to f16 with a scale of their own (11 significant bits), keys and values exact.
+ * The workspace is that of razer_attn_kv8_workspace_bytes, prepared once by razer_workspace_init; calls that may overlap on the
+ * GPU must not share one (two replayed graphs included).  razer_workspace_status reports a wait that gave up. */
+int razer_attn_kv8_workspace_bytes(const razer_kv8* cache, int q_heads, size_t* bytes_out);
+int razer_attn_kv8(const razer_kv8* cache, const void* q_dev, long long q_stride, int q_heads,
+                   const int32_t* block_table_dev, int table_width, const int32_t* q_start_dev,
+                   const int32_t* kv_len_dev, int B, int T, float scale, void* out_dev, float* lse_dev,
+                   void* workspace_dev, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
 
 import torch
 
@@ -29,6 +29,7 @@ EXPORTS = (
     "razer_workspace_bytes", "razer_workspace_init", "razer_workspace_status", "razer_gemv", "razer_gemm", "razer_gemv_host", "razer_quant_act",
     "razer_decode_act", "razer_gemm_w4a4", "razer_gemv_static", "razer_quant_weight",
     "razer_fp4_act_bytes", "razer_quant_act_fp4", "razer_gemm_w4a4_fp4",
+    "razer_quant_i8", "razer_gemm_i8", "razer_kv8_append", "razer_attn_kv8_workspace_bytes", "razer_attn_kv8",
 )
 
 
@@ -36,6 +37,12 @@ class RazerDesc(ctypes.Structure):
     """Mirror of `razer_desc` in include/razer.h."""
     _fields_ = [("N", c_int32), ("K", c_int32), ("block", c_int32), ("scale_fmt", c_int32),
                 ("remap_code", c_int32), ("sv_mag", c_float * 2), ("tensor_scale", c_float)]
+
+
+class RazerKv8(ctypes.Structure):
+    """Mirror of `razer_kv8` in include/razer.h; `tensors` (make_kv8) keeps the pools alive."""
+    _fields_ = [("pages", c_int32), ("page", c_int32), ("heads", c_int32), ("head_dim", c_int32), ("k_codes_dev", c_void_p),
+                ("v_codes_dev", c_void_p), ("k_scales_dev", c_void_p), ("v_scales_dev", c_void_p)]
 
 
 class RazerError(RuntimeError):
@@ -74,6 +81,13 @@ _lib.razer_gemm_w4a4_fp4.argtypes = [POINTER(RazerDesc), c_void_p, c_void_p, c_v
 _lib.razer_decode_act.argtypes = [c_void_p, c_void_p, c_int, c_int, c_float, c_void_p, c_void_p]
 _lib.razer_gemm_w4a4.argtypes = [POINTER(RazerDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_int,
                                  c_void_p, c_void_p, c_size_t, c_int, c_void_p]
+_lib.razer_quant_i8.argtypes = [c_void_p, c_int, c_int, c_int, c_longlong, c_void_p, c_void_p, c_void_p]
+_lib.razer_gemm_i8.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]
+_lib.razer_kv8_append.argtypes = [POINTER(RazerKv8), c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_int, c_void_p, c_void_p, c_int, c_int,
+                                  c_void_p]
+_lib.razer_attn_kv8_workspace_bytes.argtypes = [POINTER(RazerKv8), c_int, POINTER(c_size_t)]
+_lib.razer_attn_kv8.argtypes = [POINTER(RazerKv8), c_void_p, c_longlong, c_int, c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_float, c_void_p,
+                                c_void_p, c_void_p, c_size_t, c_void_p]
 for _n in EXPORTS:
     if _n not in ("razer_last_error", "razer_kernel_launches"):
         getattr(_lib, _n).restype = c_int
@@ -342,3 +356,113 @@ def razer_gemm_w4a4(desc, packed, act_codes, act_scales, act_tensor_scale, act_s
                                 _ptr(act_tensor_scale), float(act_sv_mag), M, _ptr(y), _ptr(workspace),
                                 workspace.numel(), 1 if use_native_fp4 else 0, _stream()))
     return y
+
+
+# ---- 8-bit integers: rows with a scale each, their product, and the paged cache of keys and values
+
+def _here(*tensors) -> bool:
+    """All on the current device, whose current stream the call goes to."""
+    at = torch.cuda.current_device()
+    return all(t.is_cuda and t.device.index == at for t in tensors)
+
+
+def razer_quant_i8(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None):
+    """x bf16 or FP32 [M, K] (device; rows may be a stride apart) -> (codes int8 [M, K], scales float32 [M]).  Tokens online, weight channels
+    offline."""
+    assert x.dtype in (torch.bfloat16, torch.float32) and x.dim() == 2 and x.stride(1) == 1
+    M, K = x.shape
+    if codes is None:
+        codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device=x.device)
+    assert codes.dtype == torch.int8 and codes.shape == x.shape and codes.is_contiguous()
+    assert scales.dtype == torch.float32 and scales.shape == (M,) and scales.is_contiguous()
+    assert _here(x, codes, scales)
+    _check(_lib.razer_quant_i8(_ptr(x), int(x.dtype == torch.float32), M, K, K if M == 1 else x.stride(0), _ptr(codes), _ptr(scales), _stream()))
+    return codes, scales
+
+
+def razer_gemm_i8(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+                  y: torch.Tensor | None = None) -> torch.Tensor:
+    """x_codes int8 [M, K], x_scales float32 [M], w_codes int8 [N, K], w_scales float32 [N] (device) -> y bf16 [M, N]."""
+    (M, K), N = x_codes.shape, w_codes.shape[0]
+    if y is None:
+        y = torch.empty((M, N), dtype=torch.bfloat16, device=x_codes.device)
+    assert x_codes.dtype == torch.int8 and w_codes.dtype == torch.int8 and w_codes.shape == (N, K) and x_codes.is_contiguous() and w_codes.is_contiguous()
+    assert x_scales.dtype == torch.float32 and w_scales.dtype == torch.float32 and x_scales.shape == (M,) and w_scales.shape == (N,)
+    assert x_scales.is_contiguous() and w_scales.is_contiguous() and y.dtype == torch.bfloat16 and y.shape == (M, N) and y.is_contiguous()
+    assert _here(x_codes, x_scales, w_codes, w_scales, y)
+    _check(_lib.razer_gemm_i8(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), M, N, K, _ptr(y), _stream()))
+    return y
+
+
+def make_kv8(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor) -> RazerKv8:
+    """A cache over pools that the caller owns: codes int8 [pages, heads, page, head_dim], scales float32 [pages, heads] (device)."""
+    assert k_codes.dtype == torch.int8 and v_codes.dtype == torch.int8 and k_codes.dim() == 4 and k_codes.shape == v_codes.shape
+    assert k_scales.dtype == torch.float32 and v_scales.dtype == torch.float32 and k_scales.shape == v_scales.shape == k_codes.shape[:2]
+    assert all(t.is_cuda and t.is_contiguous() and t.device == k_codes.device for t in (k_codes, v_codes, k_scales, v_scales))
+    c = RazerKv8()
+    c.pages, c.heads, c.page, c.head_dim = k_codes.shape
+    c.k_codes_dev, c.v_codes_dev, c.k_scales_dev, c.v_scales_dev = (t.data_ptr() for t in (k_codes, v_codes, k_scales, v_scales))
+    c.tensors = (k_codes, v_codes, k_scales, v_scales)
+    return c
+
+
+def _batch(cache, T, block_table, q_start, kv_len):
+    B = kv_len.shape[0]
+    assert block_table.dtype == q_start.dtype == kv_len.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == B
+    assert q_start.shape == (B + 1,) and kv_len.shape == (B,) and block_table.is_contiguous() and q_start.is_contiguous() and kv_len.is_contiguous()
+    return B
+
+
+def _rows(x, heads, head_dim):
+    """bf16 [T, heads, head_dim] with tokens a stride apart, a token's values side by side; that stride."""
+    assert x.dtype == torch.bfloat16 and x.dim() == 3 and x.shape[1:] == (heads, head_dim) and x.stride(2) == 1 and (heads == 1 or x.stride(1) == head_dim)
+    return x.stride(0) if x.shape[0] > 1 else heads * head_dim
+
+
+def razer_kv8_append(cache: RazerKv8, k_new: torch.Tensor, v_new: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor,
+                     kv_len: torch.Tensor) -> None:
+    """k_new, v_new bf16 [T, heads, head_dim] (columns of a wider matrix serve), block_table int32 [B, width], q_start int32 [B + 1],
+    kv_len int32 [B], the new tokens included (all device)."""
+    T = k_new.shape[0]
+    B = _batch(cache, T, block_table, q_start, kv_len)
+    assert v_new.shape[0] == T and _here(cache.tensors[0], k_new, v_new, block_table, q_start, kv_len)
+    k_stride, v_stride = _rows(k_new, cache.heads, cache.head_dim), _rows(v_new, cache.heads, cache.head_dim)
+    _check(_lib.razer_kv8_append(ctypes.byref(cache), _ptr(k_new), k_stride, _ptr(v_new), v_stride, _ptr(block_table), block_table.shape[1], _ptr(q_start),
+                                 _ptr(kv_len), B, T, _stream()))
+
+
+def razer_attn_kv8_workspace_bytes(cache: RazerKv8, q_heads: int) -> int:
+    n = c_size_t()
+    _check(_lib.razer_attn_kv8_workspace_bytes(ctypes.byref(cache), int(q_heads), ctypes.byref(n)))
+    return n.value
+
+
+def alloc_attn_workspace(cache: RazerKv8, q_heads: int, device) -> torch.Tensor:
+    """Allocate (torch) and prepare (razer_workspace_init) a workspace for razer_attn_kv8; it serves any batch."""
+    ws = torch.empty(razer_attn_kv8_workspace_bytes(cache, q_heads), dtype=torch.uint8, device=device)
+    razer_workspace_init(ws)
+    return ws
+
+
+def razer_attn_kv8(cache: RazerKv8, q: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                   scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None):
+    """q bf16 [T, q_heads, head_dim] (columns of a wider matrix serve) -> (out bf16 [T, q_heads, head_dim], lse float32 [T, q_heads]); the batch as
+    in razer_kv8_append, scale 1 / sqrt(head_dim) where none is given.  Rows that no sequence owns are left as they are."""
+    T, q_heads = q.shape[0], q.shape[1]
+    B = _batch(cache, T, block_table, q_start, kv_len)
+    q_stride = _rows(q, q_heads, cache.head_dim)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if lse is None:
+        lse = torch.empty((T, q_heads), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = alloc_attn_workspace(cache, q_heads, q.device)
+    assert out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (T, q_heads)
+    assert lse.is_contiguous() and _here(cache.tensors[0], q, block_table, q_start, kv_len, out, lse, workspace)
+    _check(_lib.razer_attn_kv8(ctypes.byref(cache), _ptr(q), q_stride, q_heads, _ptr(block_table), block_table.shape[1], _ptr(q_start), _ptr(kv_len), B, T,
+                               cache.head_dim ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
+                               _stream()))
+    return out, lse

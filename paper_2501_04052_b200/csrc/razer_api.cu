@@ -7,6 +7,7 @@
 #include <cstdlib>
 
 #include "razer_common.cuh"
+#include "razer_kv8.cuh"
 
 namespace razer {
 
@@ -91,6 +92,11 @@ int launch_gemv_stream(const razer_desc*, const void* packed, const void* x, int
                        const float* extra_scale_dev, void* y, void* ws, size_t ws_bytes, cudaStream_t, uint32_t* status_host);
 size_t gemv_stream_workspace_bytes(const razer_desc*, int M);
 bool gemv_stream_supported(const razer_desc*, int M);
+int launch_quant_i8(const void*, int x_is_fp32, int M, int K, long long row_stride, int8_t*, float*, cudaStream_t);
+int launch_gemm_i8(const int8_t* x, const float* sx, const int8_t* w, const float* sw, int M, int N, int K, void* y, cudaStream_t);
+int launch_kv8_append(const Kv8&, const Kv8Batch&, const void* k_new, const void* v_new, long long k_stride, long long v_stride, cudaStream_t);
+int launch_attn_kv8(const Kv8&, const Kv8Batch&, const void* q, long long q_stride, int q_heads, float scale, void* out, float* lse, void* ws, cudaStream_t);
+size_t attn_kv8_workspace_bytes(int head_dim);
 
 // Kernel choice.  M <= 8 (one group of tokens along the MMA's n) goes to the TMA-fed register-fragment kernel
 // (razer_gemv_stream.cu), whose fixed cost per launch is small (1024 x 1024: 2.2 us against 3.6) and which decodes faster (8 x 4096 x 4096
@@ -430,6 +436,110 @@ int razer_gemm_w4a4(const razer_desc* d, const void* packed_w_dev, const uint8_t
   RAZER_TRY(razer_decode_act(act_codes_dev, act_scales_dev, M, d->K, act_sv_mag, act, stream));
   return matmul_common(d, packed_w_dev, act, M, y_dev, workspace_dev, own_bytes, 1.0f, act_tensor_scale_dev,
                        (cudaStream_t)stream);
+}
+
+int razer_quant_i8(const void* x_dev, int x_is_fp32, int M, int K, long long row_stride, int8_t* codes_dev, float* scales_dev, void* stream) {
+  if (M < 1 || K < 16 || K % 16) return set_error(RAZER_ERR_INVALID_ARG, "M=%d K=%d invalid (K %% 16 == 0)", M, K);
+  const int per = x_is_fp32 ? 4 : 8;
+  if (row_stride < K || row_stride % per || row_stride > (1ll << 40))
+    return set_error(RAZER_ERR_INVALID_ARG, "row stride %lld of K=%d columns (at least K, rows 16-byte aligned)", row_stride, K);
+  RAZER_TRY(check_ptr(x_dev, 16, "x_dev"));
+  RAZER_TRY(check_ptr(codes_dev, 8, "codes_dev"));
+  RAZER_TRY(check_ptr(scales_dev, 4, "scales_dev"));
+  return launch_quant_i8(x_dev, x_is_fp32 ? 1 : 0, M, K, row_stride, codes_dev, scales_dev, (cudaStream_t)stream);
+}
+
+int razer_gemm_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev, const float* w_scales_dev, int M, int N, int K,
+                  void* y_dev, void* stream) {
+  if (M < 1 || N < 1 || K < 16 || K % 16) return set_error(RAZER_ERR_INVALID_ARG, "M=%d N=%d K=%d invalid (K %% 16 == 0)", M, N, K);
+  if (K > 131056) return set_error(RAZER_ERR_UNSUPPORTED, "K=%d: the sum would not fit 32 bits (K <= 131056)", K);
+  RAZER_TRY(check_ptr(x_codes_dev, 16, "x_codes_dev"));
+  RAZER_TRY(check_ptr(x_scales_dev, 4, "x_scales_dev"));
+  RAZER_TRY(check_ptr(w_codes_dev, 16, "w_codes_dev"));
+  RAZER_TRY(check_ptr(w_scales_dev, 4, "w_scales_dev"));
+  RAZER_TRY(check_ptr(y_dev, 2, "y_dev"));
+  return launch_gemm_i8(x_codes_dev, x_scales_dev, w_codes_dev, w_scales_dev, M, N, K, y_dev, (cudaStream_t)stream);
+}
+
+static int check_kv8(const razer_kv8* c, Kv8& out) {
+  if (!c) return set_error(RAZER_ERR_INVALID_ARG, "cache is NULL");
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
+    return set_error(RAZER_ERR_UNSUPPORTED, "page of %d tokens (16, 32, 64 and 128 are built)", c->page);
+  if (c->head_dim != 64 && c->head_dim != 128) return set_error(RAZER_ERR_UNSUPPORTED, "head dimension %d (64 and 128 are built)", c->head_dim);
+  if (c->pages < 1 || c->heads < 1 || c->heads > 32767 || (long long)c->pages * c->heads > 0x7FFFFFFFll)
+    return set_error(RAZER_ERR_INVALID_ARG, "pages=%d heads=%d out of range", c->pages, c->heads);
+  RAZER_TRY(check_ptr(c->k_codes_dev, 16, "k_codes_dev"));
+  RAZER_TRY(check_ptr(c->v_codes_dev, 16, "v_codes_dev"));
+  RAZER_TRY(check_ptr(c->k_scales_dev, 4, "k_scales_dev"));
+  RAZER_TRY(check_ptr(c->v_scales_dev, 4, "v_scales_dev"));
+  out.k = c->k_codes_dev, out.v = c->v_codes_dev, out.k_scales = c->k_scales_dev, out.v_scales = c->v_scales_dev;
+  out.pages = c->pages, out.page = c->page, out.heads = c->heads, out.D = c->head_dim;
+  out.page_log2 = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
+  return RAZER_OK;
+}
+
+static int check_batch(const razer_kv8* c, const int32_t* table, int width, const int32_t* q_start, const int32_t* kv_len, int B, int T, Kv8Batch& out) {
+  if (B < 0 || T < 0) return set_error(RAZER_ERR_INVALID_ARG, "B=%d T=%d invalid", B, T);
+  if (width < 1 || (long long)width * c->page >= 0x7FFFFFFFll - 1023)
+    return set_error(RAZER_ERR_INVALID_ARG, "block table of %d pages of %d tokens out of range", width, c->page);
+  if (B > 0 && T > 0) {
+    RAZER_TRY(check_ptr(table, 4, "block_table_dev"));
+    RAZER_TRY(check_ptr(q_start, 4, "q_start_dev"));
+    RAZER_TRY(check_ptr(kv_len, 4, "kv_len_dev"));
+  }
+  out.table = table, out.q_start = q_start, out.kv_len = kv_len, out.width = width, out.B = B, out.T = T;
+  return RAZER_OK;
+}
+
+static int check_rows(const void* p, long long stride, long long columns, const char* name) {
+  if (stride < columns || stride % 8 || stride > (1ll << 40))
+    return set_error(RAZER_ERR_INVALID_ARG, "%s: stride %lld of %lld columns (at least as many, a multiple of 8)", name, stride, columns);
+  return check_ptr(p, 16, name);
+}
+
+int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_stride, const void* v_new_dev, long long v_stride,
+                     const int32_t* block_table_dev, int table_width, const int32_t* q_start_dev, const int32_t* kv_len_dev, int B, int T, void* stream) {
+  Kv8 c;
+  Kv8Batch s;
+  RAZER_TRY(check_kv8(cache, c));
+  RAZER_TRY(check_batch(cache, block_table_dev, table_width, q_start_dev, kv_len_dev, B, T, s));
+  if (B == 0 || T == 0) return RAZER_OK;
+  RAZER_TRY(check_rows(k_new_dev, k_stride, (long long)c.heads * c.D, "k_new_dev"));
+  RAZER_TRY(check_rows(v_new_dev, v_stride, (long long)c.heads * c.D, "v_new_dev"));
+  return launch_kv8_append(c, s, k_new_dev, v_new_dev, k_stride, v_stride, (cudaStream_t)stream);
+}
+
+static int check_heads(const Kv8& c, int q_heads) {
+  if (q_heads < 1 || q_heads % c.heads) return set_error(RAZER_ERR_INVALID_ARG, "%d query heads are not a multiple of %d key-value heads", q_heads, c.heads);
+  return RAZER_OK;
+}
+
+int razer_attn_kv8_workspace_bytes(const razer_kv8* cache, int q_heads, size_t* bytes_out) {
+  Kv8 c;
+  RAZER_TRY(check_kv8(cache, c));
+  RAZER_TRY(check_heads(c, q_heads));
+  if (!bytes_out) return set_error(RAZER_ERR_INVALID_ARG, "bytes_out is NULL");
+  *bytes_out = align_up(attn_kv8_workspace_bytes(c.D), 256);
+  return RAZER_OK;
+}
+
+int razer_attn_kv8(const razer_kv8* cache, const void* q_dev, long long q_stride, int q_heads, const int32_t* block_table_dev, int table_width,
+                   const int32_t* q_start_dev, const int32_t* kv_len_dev, int B, int T, float scale, void* out_dev, float* lse_dev, void* workspace_dev,
+                   size_t workspace_bytes, void* stream) {
+  Kv8 c;
+  Kv8Batch s;
+  RAZER_TRY(check_kv8(cache, c));
+  RAZER_TRY(check_heads(c, q_heads));
+  RAZER_TRY(check_batch(cache, block_table_dev, table_width, q_start_dev, kv_len_dev, B, T, s));
+  if (!std::isfinite(scale)) return set_error(RAZER_ERR_INVALID_ARG, "scale %g is not finite", scale);
+  if (B == 0 || T == 0) return RAZER_OK;
+  RAZER_TRY(check_rows(q_dev, q_stride, (long long)q_heads * c.D, "q_dev"));
+  RAZER_TRY(check_ptr(out_dev, 16, "out_dev"));
+  if (lse_dev) RAZER_TRY(check_ptr(lse_dev, 4, "lse_dev"));
+  const size_t need = align_up(attn_kv8_workspace_bytes(c.D), 256);
+  if (!workspace_dev || workspace_bytes < need) return set_error(RAZER_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+  RAZER_TRY(check_ptr(workspace_dev, 256, "workspace_dev"));
+  return launch_attn_kv8(c, s, q_dev, q_stride, q_heads, scale, out_dev, lse_dev, workspace_dev, (cudaStream_t)stream);
 }
 
 }  // extern "C"

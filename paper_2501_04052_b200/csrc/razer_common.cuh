@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 #include <stddef.h>
+#include <atomic>
 #include <cstdlib>
 #include <utility>
 
@@ -212,23 +213,48 @@ __device__ __forceinline__ uint32_t to_packed_order(uint32_t w) {
 
 // A launch that may begin while the preceding kernel of the stream drains (programmatic dependent launch; RAZER_PDL=0 in the
 // environment, read once, turns it off): the kernel touches nothing that kernel may own before its grid_dep_wait().  `what` names it
-// in the error text.
+// in the error text; `cluster` CTAs along x form a cluster.
 template <class... P, class... A>
-inline int launch_dependent(const char* what, void (*kern)(P...), long long grid, int threads, size_t smem, cudaStream_t st, A&&... args) {
+inline int launch_dependent_clusters(const char* what, void (*kern)(P...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, A&&... args) {
   static const bool pdl = [] { const char* e = getenv("RAZER_PDL"); return !(e && e[0] == '0'); }();
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (pdl) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)cluster;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = pdl ? 1 : 0;
+  cfg.numAttrs = n;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
   count_launches(1);
   return check_cuda(e, what);
+}
+template <class... P, class... A>
+inline int launch_dependent(const char* what, void (*kern)(P...), long long grid, int threads, size_t smem, cudaStream_t st, A&&... args) {
+  return launch_dependent_clusters(what, kern, dim3((unsigned)grid), 1, threads, smem, st, std::forward<A>(args)...);
+}
+
+// A kernel's permission to use `bytes` of dynamic shared memory, asked for once on each device (`done`: a bit for each).
+inline int allow_smem(const void* kern, size_t bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  RAZER_TRY(check_cuda(cudaGetDevice(&dev), "cudaGetDevice"));
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return RAZER_OK;
+  RAZER_TRY(check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes),
+                       "cudaFuncSetAttribute(max dynamic shared memory)"));
+  if (dev < 64) done.fetch_or(bit, std::memory_order_release);
+  return RAZER_OK;
 }
 
 }  // namespace razer
