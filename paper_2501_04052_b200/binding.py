@@ -136,11 +136,15 @@ _call, _route = _load_call()
 
 
 def call_route() -> str:
-    """How razer_gemv, razer_gemm and razer_gemv_host reach the library for plain arguments."""
+    """How razer_gemv, razer_gemm, razer_gemv_host and the 8-bit calls reach the library for plain arguments."""
     return _route
 
 
 _GEMV, _GEMM, _GEMV_HOST = (ctypes.cast(f, c_void_p).value for f in (_lib.razer_gemv, _lib.razer_gemm, _lib.razer_gemv_host))
+
+
+_QUANT_I8, _GEMM_I8, _APPEND, _ATTN = (ctypes.cast(f, c_void_p).value for f in (_lib.razer_quant_i8, _lib.razer_gemm_i8, _lib.razer_kv8_append,
+                                                                                _lib.razer_attn_kv8))
 
 
 def _ptr(t) -> int:
@@ -369,6 +373,10 @@ def _here(*tensors) -> bool:
 def razer_quant_i8(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None):
     """x bf16 or FP32 [M, K] (device; rows may be a stride apart) -> (codes int8 [M, K], scales float32 [M]).  Tokens online, weight channels
     offline."""
+    if _call is not None:
+        r = _call.quant_i8(_QUANT_I8, x, codes, scales)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
     assert x.dtype in (torch.bfloat16, torch.float32) and x.dim() == 2 and x.stride(1) == 1
     M, K = x.shape
     if codes is None:
@@ -385,6 +393,10 @@ def razer_quant_i8(x: torch.Tensor, codes: torch.Tensor | None = None, scales: t
 def razer_gemm_i8(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
                   y: torch.Tensor | None = None) -> torch.Tensor:
     """x_codes int8 [M, K], x_scales float32 [M], w_codes int8 [N, K], w_scales float32 [N] (device) -> y bf16 [M, N]."""
+    if _call is not None:
+        r = _call.gemm_i8(_GEMM_I8, x_codes, x_scales, w_codes, w_scales, y)
+        if r is not None:
+            return r if type(r) is not int else _check(r)
     (M, K), N = x_codes.shape, w_codes.shape[0]
     if y is None:
         y = torch.empty((M, N), dtype=torch.bfloat16, device=x_codes.device)
@@ -425,6 +437,10 @@ def razer_kv8_append(cache: RazerKv8, k_new: torch.Tensor, v_new: torch.Tensor, 
                      kv_len: torch.Tensor) -> None:
     """k_new, v_new bf16 [T, heads, head_dim] (columns of a wider matrix serve), block_table int32 [B, width], q_start int32 [B + 1],
     kv_len int32 [B], the new tokens included (all device)."""
+    if _call is not None:
+        rc = _call.kv8_append(_APPEND, RazerKv8, cache, k_new, v_new, block_table, q_start, kv_len)
+        if rc is not None:
+            return _check(rc)
     T = k_new.shape[0]
     B = _batch(cache, T, block_table, q_start, kv_len)
     assert v_new.shape[0] == T and _here(cache.tensors[0], k_new, v_new, block_table, q_start, kv_len)
@@ -451,6 +467,10 @@ def razer_attn_kv8(cache: RazerKv8, q: torch.Tensor, block_table: torch.Tensor, 
                    workspace: torch.Tensor | None = None):
     """q bf16 [T, q_heads, head_dim] (columns of a wider matrix serve) -> (out bf16 [T, q_heads, head_dim], lse float32 [T, q_heads]); the batch as
     in razer_kv8_append, scale 1 / sqrt(head_dim) where none is given.  Rows that no sequence owns are left as they are."""
+    if workspace is not None and _call is not None:
+        r = _call.attn_kv8(_ATTN, RazerKv8, cache, q, block_table, q_start, kv_len, scale, out, lse, workspace)
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
     T, q_heads = q.shape[0], q.shape[1]
     B = _batch(cache, T, block_table, q_start, kv_len)
     q_stride = _rows(q, q_heads, cache.head_dim)

@@ -4,10 +4,13 @@
 // arguments through ctypes took as long again (1 x 1024 x 1024, host-bound: 4.9 us a call, 2.8 with this and the plans remembered).
 // matmul() and gemv_host() take the address of the library's function and the type that a descriptor must have, and return the
 // library's return code, or None for anything that is not a plain call; binding.py then takes its own way, which also raises what there
-// is to raise.  Nothing is kept between calls.
+// is to raise.  Nothing is kept between calls.  The 8-bit calls (quant_i8, gemm_i8, kv8_append, attn_kv8) return their tensors where the
+// library returns 0, and allocate those that the caller did not bring.
 #include <Python.h>
 
+#include <ATen/ATen.h>
 #include <c10/cuda/CUDAStream.h>
+#include <cmath>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/razer.h"
@@ -103,7 +106,169 @@ PyObject* gemv_host(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
-PyMethodDef methods[] = {{"matmul", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(matmul)), METH_FASTCALL, nullptr},
+// ---- 8-bit integers
+typedef int (*QuantI8Fn)(const void*, int, int, int, long long, int8_t*, float*, void*);
+typedef int (*GemmI8Fn)(const int8_t*, const float*, const int8_t*, const float*, int, int, int, void*, void*);
+typedef int (*AppendFn)(const razer_kv8*, const void*, long long, const void*, long long, const int32_t*, int, const int32_t*, const int32_t*, int, int, void*);
+typedef int (*AttnFn)(const razer_kv8*, const void*, long long, int, const int32_t*, int, const int32_t*, const int32_t*, int, int, float, void*, float*, void*, size_t,
+                      void*);
+
+// On the current device, with memory of its own.
+bool here(const at::Tensor& t, at::ScalarType type, c10::DeviceIndex dev) { return dense(t) && t.is_cuda() && t.get_device() == dev && t.scalar_type() == type; }
+bool whole(const at::Tensor& t, at::ScalarType type, c10::DeviceIndex dev, at::IntArrayRef shape) { return here(t, type, dev) && t.sizes() == shape && t.is_contiguous(); }
+bool counts(const at::Tensor& t) {
+  for (int64_t n : t.sizes())
+    if (n > INT32_MAX) return false;
+  return true;
+}
+// The caller's tensor, or a new one where `o` is None; false where it is neither.
+bool given(PyObject* o, at::Tensor& t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
+  if (o == Py_None) {
+    t = at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    return true;
+  }
+  if (!plain(o)) return false;
+  t = tensor(o);
+  return true;
+}
+PyObject* pair_of(const at::Tensor& a, const at::Tensor& b) {
+  PyObject *x = THPVariable_Wrap(a), *y = THPVariable_Wrap(b);
+  PyObject* t = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+  Py_XDECREF(x);
+  Py_XDECREF(y);
+  return t;
+}
+
+// quant_i8(function, x, codes or None, scales or None)
+PyObject* quant_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4 || !plain(a[1])) Py_RETURN_NONE;
+  const QuantI8Fn fn = reinterpret_cast<QuantI8Fn>(address(a[0]));
+  if (!fn) Py_RETURN_NONE;
+  try {
+    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream();
+    const at::Tensor& x = tensor(a[1]);
+    const bool fp32 = x.scalar_type() == at::kFloat;
+    if (!here(x, fp32 ? at::kFloat : at::kBFloat16, st.device_index()) || x.dim() != 2 || x.stride(1) != 1 || !counts(x)) Py_RETURN_NONE;
+    const int64_t M = x.size(0), K = x.size(1);
+    at::Tensor codes, scales;
+    if (!given(a[2], codes, x, at::kChar, {M, K}) || !given(a[3], scales, x, at::kFloat, {M}) || !whole(codes, at::kChar, st.device_index(), {M, K}) ||
+        !whole(scales, at::kFloat, st.device_index(), {M}))
+      Py_RETURN_NONE;
+    const int rc = fn(x.data_ptr(), fp32, (int)M, (int)K, M == 1 ? K : x.stride(0), static_cast<int8_t*>(codes.data_ptr()), static_cast<float*>(scales.data_ptr()), st.stream());
+    return rc == 0 ? pair_of(codes, scales) : PyLong_FromLong(rc);
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
+// gemm_i8(function, x codes, x scales, w codes, w scales, y or None)
+PyObject* gemm_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6 || !plain(a[1]) || !plain(a[2]) || !plain(a[3]) || !plain(a[4])) Py_RETURN_NONE;
+  const GemmI8Fn fn = reinterpret_cast<GemmI8Fn>(address(a[0]));
+  if (!fn) Py_RETURN_NONE;
+  try {
+    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream();
+    const c10::DeviceIndex dev = st.device_index();
+    const at::Tensor &x = tensor(a[1]), &sx = tensor(a[2]), &w = tensor(a[3]), &sw = tensor(a[4]);
+    if (!dense(x) || !dense(w) || x.dim() != 2 || w.dim() != 2 || !counts(x) || !counts(w)) Py_RETURN_NONE;
+    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+    at::Tensor y;
+    if (!whole(x, at::kChar, dev, {M, K}) || !whole(w, at::kChar, dev, {N, K}) || !whole(sx, at::kFloat, dev, {M}) || !whole(sw, at::kFloat, dev, {N}) ||
+        !given(a[5], y, x, at::kBFloat16, {M, N}) || !whole(y, at::kBFloat16, dev, {M, N}))
+      Py_RETURN_NONE;
+    const int rc = fn(static_cast<const int8_t*>(x.data_ptr()), static_cast<const float*>(sx.data_ptr()), static_cast<const int8_t*>(w.data_ptr()),
+                      static_cast<const float*>(sw.data_ptr()), (int)M, (int)N, (int)K, y.data_ptr(), st.stream());
+    return rc == 0 ? THPVariable_Wrap(y) : PyLong_FromLong(rc);
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
+// The cache behind binding.RazerKv8, on the current device.
+struct Cache {
+  Py_buffer view;
+  bool held = false;
+  const razer_kv8* get(PyObject* type, PyObject* o, c10::DeviceIndex dev) {
+    if (reinterpret_cast<PyObject*>(Py_TYPE(o)) != type) return nullptr;
+    PyObject* pools = PyObject_GetAttrString(o, "tensors");
+    const bool good = pools && PyTuple_Check(pools) && PyTuple_GET_SIZE(pools) == 4 && plain(PyTuple_GET_ITEM(pools, 0)) &&
+                      tensor(PyTuple_GET_ITEM(pools, 0)).is_cuda() && tensor(PyTuple_GET_ITEM(pools, 0)).get_device() == dev;
+    Py_XDECREF(pools);
+    if (!good || PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) {
+      PyErr_Clear();
+      return nullptr;
+    }
+    held = true;
+    return view.len == (Py_ssize_t)sizeof(razer_kv8) ? static_cast<const razer_kv8*>(view.buf) : nullptr;
+  }
+  ~Cache() {
+    if (held) PyBuffer_Release(&view);
+  }
+};
+// block table, q_start, kv_len of a batch
+bool batch(PyObject* const* a, c10::DeviceIndex dev) {
+  for (int i = 0; i < 3; ++i)
+    if (!plain(a[i]) || !here(tensor(a[i]), at::kInt, dev) || !tensor(a[i]).is_contiguous() || !counts(tensor(a[i]))) return false;
+  const at::Tensor &table = tensor(a[0]), &starts = tensor(a[1]), &lens = tensor(a[2]);
+  return table.dim() == 2 && starts.dim() == 1 && lens.dim() == 1 && table.size(0) == lens.size(0) && starts.size(0) == lens.size(0) + 1;
+}
+// bf16 [T, heads, head_dim], a token's values side by side
+bool rows(const at::Tensor& x, int64_t heads, int64_t D, c10::DeviceIndex dev) {
+  return here(x, at::kBFloat16, dev) && x.dim() == 3 && x.size(1) == heads && x.size(2) == D && x.stride(2) == 1 && (heads == 1 || x.stride(1) == D) && counts(x);
+}
+long long stride_of(const at::Tensor& x) { return x.size(0) > 1 ? x.stride(0) : x.size(1) * x.size(2); }
+const int32_t* ints(PyObject* o) { return static_cast<const int32_t*>(tensor(o).data_ptr()); }
+
+// kv8_append(function, cache type, cache, k, v, block table, q_start, kv_len): the library's code, or None
+PyObject* kv8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8 || !plain(a[3]) || !plain(a[4])) Py_RETURN_NONE;
+  const AppendFn fn = reinterpret_cast<AppendFn>(address(a[0]));
+  if (!fn) Py_RETURN_NONE;
+  try {
+    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream();
+    const c10::DeviceIndex dev = st.device_index();
+    Cache cache;
+    const razer_kv8* c = cache.get(a[1], a[2], dev);
+    const at::Tensor &k = tensor(a[3]), &v = tensor(a[4]);
+    if (!c || !rows(k, c->heads, c->head_dim, dev) || !rows(v, c->heads, c->head_dim, dev) || k.size(0) != v.size(0) || !batch(a + 5, dev)) Py_RETURN_NONE;
+    return PyLong_FromLong(fn(c, k.data_ptr(), stride_of(k), v.data_ptr(), stride_of(v), ints(a[5]), (int)tensor(a[5]).size(1), ints(a[6]), ints(a[7]),
+                              (int)tensor(a[7]).size(0), (int)k.size(0), st.stream()));
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
+// attn_kv8(function, cache type, cache, q, block table, q_start, kv_len, scale or None, out or None, lse or None, workspace)
+PyObject* attn_kv8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11 || !plain(a[3]) || !plain(a[10]) || (a[7] != Py_None && !PyFloat_CheckExact(a[7]))) Py_RETURN_NONE;
+  const AttnFn fn = reinterpret_cast<AttnFn>(address(a[0]));
+  if (!fn) Py_RETURN_NONE;
+  try {
+    const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream();
+    const c10::DeviceIndex dev = st.device_index();
+    Cache cache;
+    const razer_kv8* c = cache.get(a[1], a[2], dev);
+    const at::Tensor &q = tensor(a[3]), &ws = tensor(a[10]);
+    if (!c || !dense(q) || q.dim() != 3 || !rows(q, q.size(1), c->head_dim, dev) || !batch(a + 4, dev) || !here(ws, ws.scalar_type(), dev) ||
+        ws.scalar_type() != at::kByte || !ws.is_contiguous())
+      Py_RETURN_NONE;
+    const int64_t T = q.size(0), H = q.size(1), D = q.size(2);
+    at::Tensor out, lse;
+    if (!given(a[8], out, q, at::kBFloat16, {T, H, D}) || !given(a[9], lse, q, at::kFloat, {T, H}) || !whole(out, at::kBFloat16, dev, {T, H, D}) ||
+        !whole(lse, at::kFloat, dev, {T, H}))
+      Py_RETURN_NONE;
+    const float scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : (float)PyFloat_AS_DOUBLE(a[7]);
+    const int rc = fn(c, q.data_ptr(), stride_of(q), (int)H, ints(a[4]), (int)tensor(a[4]).size(1), ints(a[5]), ints(a[6]), (int)tensor(a[6]).size(0), (int)T, scale,
+                      out.data_ptr(), static_cast<float*>(lse.data_ptr()), ws.data_ptr(), (size_t)ws.numel(), st.stream());
+    return rc == 0 ? pair_of(out, lse) : PyLong_FromLong(rc);
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
+#define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {CALL(quant_i8), CALL(gemm_i8), CALL(kv8_append), CALL(attn_kv8),
+                         {"matmul", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(matmul)), METH_FASTCALL, nullptr},
                          {"gemv_host", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gemv_host)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "razer_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
