@@ -3,12 +3,12 @@
 //   s_j = scale * ks[page(j)] * <q, kq_j>   over the keys j <= p of a row at position p
 //   out = sum_j exp(s_j) vs[page(j)] vq_j / sum_j exp(s_j),   lse = log sum_j exp(s_j)
 //
-// One pass over the cache with a running maximum and sum.  A CTA has NW consumer warps and a producer warp; a work item is a tile of TK tokens
-// of one (sequence, row tile, key-value head), and all items of the batch are cut evenly among the CTAs, whatever the sequences'
-// lengths are: every CTA works its share out from q_start and kv_len, so that the host needs neither.  The producer looks pages and scales
-// up 32 at a time and brings each page's rows by TMA; stage i belongs to warp i % NW, which has a softmax of its own; the warps meet at the
-// end of a unit.  A unit that several CTAs share is put together in CTA order by the last of them to arrive (counters that
-// reset themselves, parts in the workspace).
+// One pass over the cache with a running maximum and sum.  A work item is a tile of TK tokens of one (sequence, row tile, key-value
+// head), and all items of the batch are cut evenly among the CTAs, whatever the sequences' lengths are: every CTA works its share out
+// from q_start and kv_len, so that the host needs neither.  Item i of a CTA belongs to warp i % NW, which has a ring and a softmax of
+// its own: it looks the pages up and brings their rows by TMA itself, RING tiles ahead and across the units' ends (one producer warp for all
+// took 900 cycles a tile and bounded the kernel at 2.5 TB/s).  The warps meet at the end of a unit.  A unit that several CTAs share is put together
+// in CTA order by the last of them to arrive (counters that reset themselves, parts in the workspace).
 //
 // Both products run with the cache as operand A (16 tokens x 16 dimensions, then 16 dimensions x 16 tokens) and the rows of queries as
 // the eight columns of B, so that a decode step of up to 8 query heads a key-value head wastes nothing, and O takes 32 registers for 8 rows.
@@ -45,13 +45,13 @@ struct AttnArgs {
 template <int D_, int NB_>
 struct AttnCfg {
   static constexpr int D = D_, NB = NB_, ROWS = 8 * NB_;
-  static constexpr int NW = NB_ == 1 ? 8 : 7;            // consumer warps; registers come for 4 warps at a time, and more rows need 200 of them
-  static constexpr int THREADS = 32 * (NW + 1);
+  static constexpr int NW = 8, RING = 3;                 // warps, tiles of each warp's ring
+  static constexpr int THREADS = 32 * NW;
   static constexpr int TK = D_ == 64 ? 64 : 32;          // tokens of a tile
   static constexpr int MT = TK / 16;
   static constexpr int TILE_BYTES = TK * D;
   static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
-  static constexpr int STAGES = 3 * NW;                  // a stage always serves the same warp, which has then seen all its phases
+  static constexpr int STAGES = RING * NW;
   static constexpr int HALF = D / 2;                     // columns of O that the warps put together at a time
   static constexpr int PITCH = HALF + 4;
   static constexpr int O_RING = 0;
@@ -61,7 +61,7 @@ struct AttnCfg {
   static constexpr int O_STAT = O_JOIN + NW * 8 * PITCH * 4;             // [NW][ROWS] maximum, then sum; [NW] value scale
   static constexpr int O_ROW = (O_STAT + (2 * NW * ROWS + NW) * 4 + 7) / 8 * 8;   // [ROWS] score factor in two parts; [ROWS] visible keys
   static constexpr int O_BAR = (O_ROW + 3 * ROWS * 4 + 15) / 16 * 16;
-  static constexpr int O_MISC = O_BAR + STAGES * 16;                     // words: see below
+  static constexpr int O_MISC = O_BAR + STAGES * 8;                     // words: see below
   static constexpr int SMEM_BYTES = 1024 + O_MISC + 128;
   static constexpr int PART_FLOATS = ROWS * (D + 2);                     // a part: O, maxima, sums
 };
@@ -101,7 +101,7 @@ __device__ __forceinline__ float rebase(float m, float l, float top) {
 // a quarter warp meet no bank twice in either product (64 dimensions: values twice).
 __device__ __forceinline__ int spread(int r) { return (r & 8) | ((r & 1) ? ((r & 6) ^ 4) | 1 : (r & 6)); }
 
-// A CTA's place in the work: segments, each the part of one unit that falls to it.
+// A place in a CTA's work: segments, each the part of one unit that falls to it.
 struct Walk {
   int b, row0, n, len, tiles, units, unit, tile;
   long long left;                                        // items that remain to the CTA
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
   float* stat_v = stat_l + NW * ROWS;
   float* row_scale = reinterpret_cast<float*>(sm + C::O_ROW);
   int* row_keys = reinterpret_cast<int*>(row_scale + 2 * ROWS);
-  const uint32_t bar_full = sb + C::O_BAR, bar_empty = bar_full + 8 * ST;
+  const uint32_t bar_full = sb + C::O_BAR;
   volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm + C::O_MISC);
   int* misc = reinterpret_cast<int*>(sm + C::O_MISC);    // 0 abort, 1 a flag that nobody sets, 2 sequence, 3 last to arrive, 4.. warps' sums (long long)
   long long* sums = reinterpret_cast<long long*>(misc + 6);
@@ -130,7 +130,6 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
   if (threadIdx.x == 0) {
     for (int i = 0; i < ST; ++i) {
       mbar_init(bar_full + 8 * i, 1);
-      mbar_init(bar_empty + 8 * i, 1);
     }
     misc[0] = misc[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -157,7 +156,7 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
     if (lane == 0) sums[warp] = total;
     __syncthreads();
     total = 0;
-    for (int w = 0; w <= NW; ++w) total += sums[w];
+    for (int w = 0; w < NW; ++w) total += sums[w];
   }
   const long long per = (total + gridDim.x - 1) / gridDim.x;
   const long long begin = per * blockIdx.x, end = min(begin + per, total);
@@ -180,7 +179,7 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
       __syncthreads();
       long long before = base;
       for (int w = 0; w < warp; ++w) before += sums[w];
-      for (int w = 0; w <= NW; ++w) base += sums[w];
+      for (int w = 0; w < NW; ++w) base += sums[w];
       if (before + upto - mine <= begin && begin < before + upto) {
         misc[2] = b;
         *reinterpret_cast<long long*>(misc + 4) = begin - (before + upto - mine);
@@ -198,8 +197,8 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
     at.left = end - begin;
   }
   const long long per_items = per;
-  auto count = [&]() { return (int)min((long long)(at.tiles - at.tile), at.left); };
-  auto advance = [&](int n) {                            // on to the next segment, n items further; false at the end
+  auto count = [](const Walk& at) { return (int)min((long long)(at.tiles - at.tile), at.left); };
+  auto advance = [&](Walk& at, int n) {                            // on to the next segment, n items further; false at the end
     at.left -= n;
     if (at.left <= 0) return false;
     at.tile = 0;
@@ -214,75 +213,78 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
     return true;
   };
   // keys that the last row of the unit's row tile sees
-  auto unit_keys = [&](int qt) { return max(at.len - at.n + min((qt + 1) * a.tq, at.n), 0); };
+  auto unit_keys = [&](const Walk& at, int qt) { return max(at.len - at.n + min((qt + 1) * a.tq, at.n), 0); };
   auto fail = [&](uint32_t code) {
     *abort_flag = 1;
     atomicCAS(a.status, 0u, code);
   };
 
-  if (warp == NW) {
-    // ===================== producer =====================
-    const int rows_of_box = min(a.c.page, TK), boxes = TK / rows_of_box;
-    int item = 0;                                        // stages so far
-    bool alive = true;
-    do {
-      const int n = count(), qt = at.unit / heads, h = (at.unit - qt * heads) / a.chunks;
-      const int keys = unit_keys(qt), last = min(at.tile + n, (keys + TK - 1) / TK);
-      int have = -64, id = -1;                           // first block of the 32 that the lanes hold, and each lane's
-      float ks = 0, vs = 0;
-      for (int t = at.tile; alive && t < last; ++t) {
-        const int block0 = (t * TK) >> a.c.page_log2;
-        if (block0 + boxes > have + 32) {
-          have = block0;
-          const int block = have + lane;
-          id = -1;
-          if (((long long)block << a.c.page_log2) < keys) id = kv8_page(a.c, a.s, at.b, block);
-          ks = vs = __uint_as_float(0x7FC00000u);
-          if (id >= 0) {
-            ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + h);
-            vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + h);
-          }
-        }
-        const int stage = item % ST;
-        if (item >= ST && !mbar_wait(bar_empty + 8 * stage, (uint32_t)((item / ST) & 1) ^ 1u, abort_flag)) {
-          fail(1);
-          alive = false;
-        }
-        alive = __all_sync(0xFFFFFFFFu, alive);
-        if (!alive) break;
-        {
-          const int from = min(((t * TK + min(lane, MT - 1) * 16) >> a.c.page_log2) - have, 31);
-          const float k1 = __shfl_sync(0xFFFFFFFFu, ks, from), v1 = __shfl_sync(0xFFFFFFFFu, vs, from);
-          if (lane < MT) meta[stage * MT + lane] = make_float2(k1, v1);
-        }
-        __syncwarp();
-        const uint32_t st = sb + C::O_RING + stage * C::STAGE_BYTES, bar = bar_full + 8 * stage;
-        const int live = min(boxes, ((keys - t * TK - 1) / rows_of_box) + 1);       // boxes with a visible key
-        if (lane == 0) mbar_expect_tx(bar, (uint32_t)(live * rows_of_box * D * 2));
-        __syncwarp();
-        const int page = __shfl_sync(0xFFFFFFFFu, id, min(block0 + min(lane, live - 1) - have, 31));
-        if (lane < live) {
-          const int z = max(page, 0) * a.c.heads + h, y = (t * TK + lane * rows_of_box) & (a.c.page - 1);
-          const uint32_t to = st + (uint32_t)(lane * rows_of_box * D);
-          tma_load_3d(to, &map_k, 0, y, z, bar);
-          tma_load_3d(to + C::TILE_BYTES, &map_v, 0, y, z, bar);
-        }
-        __syncwarp();
-        ++item;
+  // ---- the warp's own loads, ahead of its sums: place in the work, the segment's tiles, the next of them for this warp
+  Walk ld = at;
+  const int rows_of_box = min(a.c.page, TK), boxes = TK / rows_of_box;
+  int ld_base = 0, ld_i = warp, ld_n = 0, ld_tile = 0, ld_keys = 0, ld_head = 0;   // the CTA's items before the segment; tile ld_i of its ld_n
+  bool ld_more = true;
+  auto segment = [&]() {
+    const int qt = ld.unit / heads;
+    ld_head = (ld.unit - qt * heads) / a.chunks;
+    ld_keys = unit_keys(ld, qt);
+    ld_tile = ld.tile;
+    ld_n = max(min(ld.tile + count(ld), (ld_keys + TK - 1) / TK) - ld.tile, 0);
+  };
+  auto settle = [&]() {                                  // to a segment that has the tile
+    while (ld_i >= ld_n) {
+      ld_i -= ld_n;
+      if (!advance(ld, count(ld))) { ld_more = false; return; }
+      segment();
+    }
+  };
+  int ld_page = 0;                                       // lane i: the page of the next tile's box i
+  auto look_up = [&]() {
+    const int tok = (ld_tile + ld_i) * TK + lane * rows_of_box;
+    ld_page = ld_more && lane < boxes && tok < ld_keys ? kv8_page(a.c, a.s, ld.b, tok >> a.c.page_log2) : -1;
+  };
+  int ld_count = 0;                                      // tiles asked for
+  float new_k = 0.0f, new_v = 0.0f;                      // lane i: scales of box i of the last of them, on their way
+  // Asks for the next tile, and puts down the scales of the one before, which have come by now.
+  auto load_next = [&]() {
+    if (ld_count > 0) {
+      const int before = warp * C::RING + (ld_count - 1) % C::RING, from = lane * 16 / rows_of_box;
+      const float k1 = __shfl_sync(0xFFFFFFFFu, new_k, from & 31), v1 = __shfl_sync(0xFFFFFFFFu, new_v, from & 31);
+      if (lane < MT) meta[before * MT + lane] = make_float2(k1, v1);
+    }
+    if (!ld_more) return;
+    const int stage = warp * C::RING + ld_count % C::RING, tok0 = (ld_tile + ld_i) * TK;
+    const uint32_t bar = bar_full + 8 * stage;
+    const int live = min(boxes, (ld_keys - tok0 - 1) / rows_of_box + 1);         // boxes with a visible key
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(live * rows_of_box * D * 2));
+    __syncwarp();
+    if (lane < live) {
+      const int z = max(ld_page, 0) * a.c.heads + ld_head, y = (tok0 + lane * rows_of_box) & (a.c.page - 1);
+      const uint32_t to = sb + C::O_RING + stage * C::STAGE_BYTES + (uint32_t)(lane * rows_of_box * D);
+      tma_load_3d(to, &map_k, 0, y, z, bar);
+      tma_load_3d(to + C::TILE_BYTES, &map_v, 0, y, z, bar);
+      new_k = new_v = __uint_as_float(0x7FC00000u);
+      if (ld_page >= 0) {
+        new_k = __ldg(a.c.k_scales + (long long)ld_page * a.c.heads + ld_head);
+        new_v = __ldg(a.c.v_scales + (long long)ld_page * a.c.heads + ld_head);
       }
-      if (!advance(n)) break;
-    } while (alive);
-    // copies still in flight must land before the CTA's shared memory is released
-    for (int f = max(item - ST, 0); f < item; ++f) mbar_wait(bar_full + 8 * (f % ST), (uint32_t)((f / ST) & 1), (volatile uint32_t*)(misc + 1));
-    return;
-  }
+    }
+    __syncwarp();
+    ++ld_count;
+    ld_i += NW;
+    settle();
+    look_up();
+  };
+  segment();
+  settle();
+  look_up();
+  for (int i = 0; i < C::RING; ++i) load_next();
 
-  // ===================== consumers =====================
   const int g = lane >> 2, t4 = lane & 3;
-  int item = 0;                                          // the CTA's stages before this segment
+  int item = 0, used = 0;                                // the CTA's items before this segment; the warp's own so far
   for (;;) {
-    const int n_items = count(), qt = at.unit / heads, hc = at.unit - qt * heads, h = hc / a.chunks, chunk = hc - h * a.chunks;
-    const int keys = unit_keys(qt), first_tile = at.tile, last = min(at.tile + n_items, (keys + TK - 1) / TK);
+    const int n_items = count(at), qt = at.unit / heads, hc = at.unit - qt * heads, h = hc / a.chunks, chunk = hc - h * a.chunks;
+    const int keys = unit_keys(at, qt), first_tile = at.tile, last = min(at.tile + n_items, (keys + TK - 1) / TK);
     // ---- the rows of queries: f16, in the order of B's fragments; row r is token r / Gc, head r % Gc of the row tile
     {
       threads_meet<32 * NW>();                                  // the unit before is done with what follows
@@ -344,8 +346,9 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
 
     const int n_stages = max(last - first_tile, 0);
     for (int i = (warp - item % NW + NW) % NW; i < n_stages; i += NW) {
-      const int it = item + i, stage = it % ST, tok0 = (first_tile + i) * TK;
-      if (!mbar_wait(bar_full + 8 * stage, (uint32_t)((it / ST) & 1), abort_flag)) fail(2);
+      const int stage = warp * C::RING + used % C::RING, tok0 = (first_tile + i) * TK;
+      if (!mbar_wait(bar_full + 8 * stage, (uint32_t)((used / C::RING) & 1), abort_flag)) fail(1);
+      ++used;
       __syncwarp();
       const uint32_t kt = sb + C::O_RING + stage * C::STAGE_BYTES, vt = kt + C::TILE_BYTES;
       // ---- S = K Q^T
@@ -468,8 +471,8 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
           for (int nb = 0; nb < NB; ++nb) mma_f16(o[j][nb], a0, a1, a2, a3, pb[mt][nb][0], pb[mt][nb][1]);
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_empty + 8 * stage);
+      __syncwarp();                                      // the tile has been read
+      load_next();
     }
     item += n_stages;
 
@@ -581,8 +584,12 @@ __global__ void __launch_bounds__(AttnCfg<D, NB>::THREADS, 1) attn_kv8_kernel(co
         }
       }
     }
-    if (!advance(n_items)) break;
+    if (!advance(at, n_items)) break;
   }
+  // after a wait that gave up: copies still in flight must land before the CTA's shared memory is released
+  if (*abort_flag)
+    for (int f = max(ld_count - C::RING, 0); f < ld_count; ++f)
+      mbar_wait(bar_full + 8 * (warp * C::RING + f % C::RING), (uint32_t)((f / C::RING) & 1), (volatile uint32_t*)(misc + 1));
 }
 
 // A tensor map over a pool of codes: (dimension, token of the page, page and head).
