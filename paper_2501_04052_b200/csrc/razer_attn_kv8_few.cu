@@ -1,0 +1,540 @@
+// Attention over the paged 8-bit cache for few rows of queries a key-value head (decoding): up to 32 of them at a time.
+//
+// The cache goes to the tensor core as it lies: keys and values are operand A of integer MMAs (tcgen05 kind::i8), brought by TMA and
+// never converted.  Queries and probabilities are operand B, split into 8-bit digits that are columns of their own:
+//   S[token][row, digit] = K Q^T    q = 2^(e - 21) (65536 d2 + 256 d1 + d0), signed digits, e from the row's largest magnitude
+//   O[dim][row, digit]   = V^T P    w = exp2(s + log2 vs - top) <= 1 held as 24 bits, three unsigned digits, top the tile's own maximum
+// The sums are exact in 32 bits, so that what is rounded is q to 2^-23 of its row's largest (bf16 queries exactly but for those below 2^-14
+// of it), w to 2^-25 of the tile's largest, and the FP32 arithmetic between.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each
+// dimension for O.  Since the digits ride along as columns (32 of S and of O for 8 rows, against 54 cycles that an MMA takes at any
+// width up to 64), they cost nothing, and a tile takes a third of the instructions that unpacking codes for mma.sync took.
+//
+// Roles: a warp each brings keys and values (pages and scales looked up 32 at a time), one prepares the queries of the next unit, one issues
+// MMAs, and GROUPS groups of four warps take the tiles in turn: maximum over the tile (nine shuffles for eight rows, then the four warps
+// through shared memory), exponentials, digits to shared memory, and O = O f + O_tile in FP32 registers.  Work is cut evenly
+// among the CTAs as razer_attn_kv8.cuh says.
+#include "razer_attn_kv8.cuh"
+
+namespace razer {
+
+namespace {
+
+constexpr float W_ONE = 16777215.0f;                                   // what a weight of 1 is held as: 24 bits
+
+template <int D_, int R_>
+struct FewCfg {
+  static constexpr int D = D_, R = R_, CHUNKS = R_ / 8;
+  static constexpr int TK = 128;
+  static constexpr int GROUPS = R_ == 8 ? 3 : 2;                     // registers: 128 a thread with three groups, 168 with two
+  static constexpr int W_K = 4 * GROUPS, W_V = W_K + 1, W_Q = W_K + 2, W_MMA = W_K + 3;       // the service warps
+  static constexpr int THREADS = 32 * (W_K + 4);
+  static constexpr int TILE_BYTES = TK * D, STAGE_BYTES = 2 * TILE_BYTES;
+  static constexpr int NS = R_ == 8 ? 32 : 3 * R_, NP = NS;                                // columns of S and of O
+  static constexpr int Q_BYTES = NS * D, P_BYTES = NP * TK;
+  static constexpr int STAGES = (D_ == 64 ? 2 : 1) * (R_ <= 16 ? 6 : 5);
+  static constexpr int O_RING = 0;
+  static constexpr int O_Q = STAGES * STAGE_BYTES;                     // two buffers, [column][D]
+  static constexpr int O_P = (O_Q + 2 * Q_BYTES + 1023) / 1024 * 1024; // [group][column][128]
+  static constexpr int JOIN_BYTES = GROUPS * 8 * D * 4;                // [group][8 rows][D] floats, over the digits where they have the room:
+  static constexpr bool JOIN_ON_P = JOIN_BYTES <= GROUPS * P_BYTES;    // at a unit's end they have been read
+  static constexpr int O_JOIN = JOIN_ON_P ? O_P : O_P + GROUPS * P_BYTES;
+  static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][2][4 warps][R]
+  static constexpr int O_STAT = O_RED + GROUPS * 8 * R * 4;            // [group][R] A, M; [group][4][R] sums
+  static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][R][8] what a tile means for each row
+  static constexpr int O_ROW = O_TABLE + 4 * GROUPS * R * 32;          // [2][R] score factor in two parts; [2][R] keys
+  static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] key scales, then value scales
+  static constexpr int O_BAR = O_META + STAGES * 64;
+  static constexpr int N_BAR = 3 * STAGES + 3 * GROUPS + 5;
+  static constexpr int O_MISC = O_BAR + 8 * N_BAR;                     // words: abort, never set, share (4 words), TMEM, last, broken values by group, sums
+  static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
+  static constexpr int S_COLS = NS <= 32 ? 32 : NS <= 64 ? 64 : 128, P_COLS = S_COLS;
+  static constexpr int TMEM_COLS = GROUPS * (S_COLS + P_COLS) <= 256 ? 256 : 512;
+  static constexpr int PART_FLOATS = R * (D + 3);                      // a part of a unit: O, A, M, sum
+};
+
+// The largest of each of eight values over a warp: nine shuffles; lane gets that of value 4 bit4 + 2 bit3 + bit2 of its number.
+template <class Op>
+__device__ __forceinline__ float reduce8(const float (&v)[8], int lane, Op op) {
+  float a[4], b[2];
+  const bool h4 = lane & 16, h3 = lane & 8, h2 = lane & 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = op(h4 ? v[4 + i] : v[i], __shfl_xor_sync(0xFFFFFFFFu, h4 ? v[i] : v[4 + i], 16));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) b[i] = op(h3 ? a[2 + i] : a[i], __shfl_xor_sync(0xFFFFFFFFu, h3 ? a[i] : a[2 + i], 8));
+  float c = op(h2 ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, h2 ? b[0] : b[1], 4));
+  c = op(c, __shfl_xor_sync(0xFFFFFFFFu, c, 2));
+  return op(c, __shfl_xor_sync(0xFFFFFFFFu, c, 1));
+}
+__device__ __forceinline__ int reduce8_row(int lane) { return ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1); }
+
+__device__ __forceinline__ void mma_digits(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 ad, bd;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "mov.b64 ad, {%1, %2};\n\t"
+      "mov.b64 bd, {%3, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], ad, bd, %5, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void sts8(uint32_t addr, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+
+template <int D, int R>
+__global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                                                const __grid_constant__ AttnArgs a) {
+  using C = FewCfg<D, R>;
+  constexpr int TK = C::TK, ST = C::STAGES, GROUPS = C::GROUPS, CHUNKS = C::CHUNKS, SOFT = 128 * GROUPS;
+  extern __shared__ uint8_t attn_smem[];
+  uint8_t* sm = attn_smem + ((1024 - (smem_u32(attn_smem) & 1023)) & 1023);
+  const uint32_t sb = smem_u32(sm);
+  const uint32_t bar_kfull = sb + C::O_BAR, bar_vfull = bar_kfull + 8 * ST, bar_empty = bar_vfull + 8 * ST, bar_sfull = bar_empty + 8 * ST,
+                 bar_pfull = bar_sfull + 8 * GROUPS, bar_ofull = bar_pfull + 8 * GROUPS, bar_qfull = bar_ofull + 8 * GROUPS, bar_qempty = bar_qfull + 16, bar_drain = bar_qempty + 16;
+  int* misc = reinterpret_cast<int*>(sm + C::O_MISC);
+  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(misc);
+  volatile uint32_t* never = reinterpret_cast<uint32_t*>(misc + 1);
+  uint32_t* broken = reinterpret_cast<uint32_t*>(misc + 8);              // [group] rows that saw a value scale that is none
+  float* meta_k = reinterpret_cast<float*>(sm + C::O_META);
+  float* meta_v = meta_k + 8 * ST;
+  float2* row_scale = reinterpret_cast<float2*>(sm + C::O_ROW);           // [2][R]
+  int* row_keys = reinterpret_cast<int*>(row_scale + 2 * R);              // [2][R]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(bar_kfull + 8 * i, 1);
+      mbar_init(bar_vfull + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < GROUPS; ++i) {
+      mbar_init(bar_sfull + 8 * i, 1);
+      mbar_init(bar_pfull + 8 * i, 128);
+      mbar_init(bar_ofull + 8 * i, 1);
+      broken[i] = 0;
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_qfull + 8 * i, 32);
+      mbar_init(bar_qempty + 8 * i, 1);
+    }
+    mbar_init(bar_drain, 1);
+    misc[0] = misc[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+  }
+  if (warp == C::W_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc + 6)), "r"((uint32_t)C::TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  grid_dep_wait();
+  grid_dep_launch();
+  long long begin, end, per;
+  Walk at;
+  const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at);   // barriers inside
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)misc[6];
+  const int heads = a.c.heads * a.chunks;
+  auto fail = [&](uint32_t code) {
+    *abort_flag = 1;
+    atomicCAS(a.status, 0u, code);
+  };
+  // a segment: tiles first .. last - 1 of a unit that have a key that anyone sees
+  struct Seg { int n_items, qt, h, chunk, keys, first, last; };
+  auto segment = [&](const Walk& at) {
+    Seg g;
+    g.n_items = walk_count(at);
+    g.qt = at.unit / heads;
+    const int hc = at.unit - g.qt * heads;
+    g.h = hc / a.chunks;
+    g.chunk = hc - g.h * a.chunks;
+    g.keys = max(at.len - at.n + min((g.qt + 1) * a.tq, at.n), 0);
+    g.first = at.tile;
+    g.last = max(min(at.tile + g.n_items, (g.keys + TK - 1) / TK), g.first);
+    return g;
+  };
+
+  if (!work) {
+  } else if (warp == C::W_K || warp == C::W_V) {
+    // ===================== keys, values =====================
+    const bool value = warp == C::W_V;
+    const CUtensorMap* map = value ? &map_v : &map_k;
+    const uint32_t bar_full = value ? bar_vfull : bar_kfull, to0 = sb + C::O_RING + (value ? C::TILE_BYTES : 0);
+    const int boxes = TK >> a.c.page_log2;                       // pages of a tile
+    int item = 0;
+    bool alive = true;
+    do {
+      const Seg g = segment(at);
+      int have = -64, id = -1, id_next = -1;                     // first of the 32 blocks that the lanes hold; the lane's page of these and of the next 32
+      float ks = 0, vs = 0;                                      // the values' warp brings both kinds of scales
+      auto page_of = [&](int block) { return ((long long)block << a.c.page_log2) < g.keys ? kv8_page(a.c, a.s, at.b, block) : -1; };
+      for (int t = g.first; t < g.last; ++t, ++item) {
+        const int block0 = t * boxes, stage = item % ST;
+        if (block0 + boxes > have + 32) {
+          id = block0 == have + 32 ? id_next : page_of(block0 + lane);
+          have = block0;
+          id_next = page_of(have + 32 + lane);
+          ks = vs = __uint_as_float(0x7FC00000u);
+          if (value && id >= 0) {
+            ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + g.h);
+            vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
+          }
+        }
+        if (item >= ST && !mbar_wait(bar_empty + 8 * stage, (uint32_t)((item / ST) & 1) ^ 1u, abort_flag)) {
+          fail(1);
+          alive = false;
+        }
+        alive = __all_sync(0xFFFFFFFFu, alive);
+        if (!alive) break;
+        const uint32_t bar = bar_full + 8 * stage;
+        const int live = min(boxes, ((g.keys - t * TK - 1) >> a.c.page_log2) + 1);
+        const int page = __shfl_sync(0xFFFFFFFFu, id, (block0 - have + lane) & 31);
+        if (value) {
+          const float k1 = __shfl_sync(0xFFFFFFFFu, ks, (block0 - have + lane) & 31), v1 = __shfl_sync(0xFFFFFFFFu, vs, (block0 - have + lane) & 31);
+          if (lane < boxes) meta_k[stage * 8 + lane] = k1, meta_v[stage * 8 + lane] = v1;
+          __syncwarp();
+        }
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)((live << a.c.page_log2) * D));
+        __syncwarp();
+        if (lane < live)
+          tma_load_3d(to0 + stage * C::STAGE_BYTES + (uint32_t)((lane << a.c.page_log2) * D), map, 0, 0, max(page, 0) * a.c.heads + g.h, bar);
+        __syncwarp();
+      }
+      if (!walk_advance(a, TK, at, g.n_items)) break;
+    } while (alive);
+    // copies in flight must land before shared memory is released
+    for (int f = max(item - ST, 0); f < item; ++f) mbar_wait(bar_full + 8 * (f % ST), (uint32_t)((f / ST) & 1), never);
+  } else if (warp == C::W_Q) {
+    // ===================== queries of the next unit =====================
+    for (int n = 0;; ++n) {
+      const Seg g = segment(at);
+      const int buf = n & 1;
+      if (n >= 2 && !mbar_wait(bar_qempty + 8 * buf, (uint32_t)((n >> 1) & 1) ^ 1u, abort_flag)) { fail(2); break; }
+      __syncwarp();
+      const bool over = kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
+      for (int c = 0; c < CHUNKS; ++c) {
+        uint32_t raw[8][D / 64];
+        bool real[8];
+        int keys[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int r = 8 * c + j, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
+          real[j] = r < a.tq * a.Gc && i < at.n && hq < a.G;
+          keys[j] = real[j] ? max(at.len - at.n + i + 1, 0) : 0;
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + lane * (D / 64);
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) raw[j][k] = real[j] ? src[k] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) top = max(top, max((raw[j][k] & 0x7FFFu) << 16, raw[j][k] & 0x7FFF0000u));
+          top = __reduce_max_sync(0xFFFFFFFFu, top);
+          const bool bad = top >= 0x7F800000u || over;
+          const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
+          const float up0 = power2((21 - e) / 2), up1 = power2(21 - e - (21 - e) / 2);
+          const int row = buf * R + 8 * c + j;
+          if (lane == 0) {
+            row_scale[row] = make_float2(bad ? __uint_as_float(0x7FC00000u) : a.scale * LOG2E * power2(e / 2), power2(e - e / 2 - 21));
+            row_keys[row] = keys[j];
+          }
+          uint32_t digit[3] = {0, 0, 0};                          // D / 32 dimensions, a byte each
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) {
+            const float x = __uint_as_float((k & 1) ? raw[j][k / 2] & 0xFFFF0000u : raw[j][k / 2] << 16);
+            int v = bad ? 0 : __float2int_rn(x * up0 * up1);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              const int lo = (int)(int8_t)v;
+              digit[q] |= (uint32_t)(lo & 255) << (8 * k);
+              v = (v - lo) >> 8;
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < 3; ++q) {
+            const int col = 24 * c + 8 * q + j, d = lane * (D / 32);
+            const uint32_t chunk16 = D == 64 ? (d >> 4) ^ ((col >> 1) & 3) : (d >> 4) ^ (col & 7);
+            const uint32_t to = sb + C::O_Q + buf * C::Q_BYTES + col * D + chunk16 * 16 + (d & 15);
+            if (D == 64) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((uint16_t)digit[q]) : "memory");
+            else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(digit[q]) : "memory");
+          }
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(bar_qfull + 8 * buf);
+      if (!walk_advance(a, TK, at, g.n_items)) break;
+    }
+  } else if (warp == C::W_MMA) {
+    // ===================== MMAs =====================
+    if (elect_one()) {
+      constexpr uint32_t hi_row = D == 64 ? (512u >> 4) | (1u << 14) | (4u << 29) : (1024u >> 4) | (1u << 14) | (2u << 29);   // rows of D bytes in their swizzle
+      constexpr uint32_t hi_p = (1024u >> 4) | (1u << 14) | (2u << 29);
+      // S32 sums; keys x query digits, both signed; values (dimension-major, M = D) signed x probability digits unsigned
+      constexpr uint32_t id_s = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(C::NS >> 3) << 17) | (8u << 24);
+      constexpr uint32_t id_p = (2u << 4) | (1u << 7) | (1u << 15) | ((uint32_t)(C::NP >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
+      auto lo = [](uint32_t addr) { return (addr >> 4) | (1u << 16); };
+      int item = 0, weighed = 0, unit_first = 0;                 // next S; next product with values, at most GROUPS behind; the segment's first
+      bool alive = true;
+      auto wait = [&](uint32_t bar, int phase, uint32_t code) {
+        if (alive && !mbar_wait(bar, (uint32_t)(phase & 1), abort_flag)) { fail(code); alive = false; }
+        return alive;
+      };
+      auto weigh_values = [&](int i) {
+        const int g = i % GROUPS, stage = i % ST;
+        if (!wait(bar_pfull + 8 * g, i / GROUPS, 3) || !wait(bar_vfull + 8 * stage, i / ST, 4)) return;
+        tc_fence_after();
+        const uint32_t v = sb + C::O_RING + stage * C::STAGE_BYTES + C::TILE_BYTES, p = sb + C::O_P + g * C::P_BYTES;
+#pragma unroll
+        for (int k = 0; k < TK / 32; ++k)
+          mma_digits(tmem + GROUPS * C::S_COLS + g * C::P_COLS, lo(v + k * 32 * D), hi_row, lo(p + k * 32), hi_p, id_p, k > 0);
+        tc_commit(bar_ofull + 8 * g);
+        tc_commit(bar_empty + 8 * stage);
+      };
+      for (int n = 0; alive; ++n) {
+        const Seg s = segment(at);
+        // The queries' buffer is free once the segment before the last is finished, which wants all of its products.  A segment without tiles waits
+        // too: a wait for one phase is sound only for who knows the one before to be over.
+        while (alive && weighed < unit_first) weigh_values(weighed++);
+        wait(bar_qfull + 8 * (n & 1), n >> 1, 5);
+        unit_first = item;
+        for (int t = s.first; alive && t < s.last; ++t, ++item) {
+          if (item - weighed >= GROUPS) weigh_values(weighed++);
+          const int g = item % GROUPS, stage = item % ST;
+          if (!wait(bar_kfull + 8 * stage, item / ST, 6)) break;
+          tc_fence_after();
+          const uint32_t k0 = sb + C::O_RING + stage * C::STAGE_BYTES, q0 = sb + C::O_Q + (n & 1) * C::Q_BYTES;
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) mma_digits(tmem + g * C::S_COLS, lo(k0 + k * 32), hi_row, lo(q0 + k * 32), hi_row, id_s, k > 0);
+          tc_commit(bar_sfull + 8 * g);
+        }
+        if (!walk_advance(a, TK, at, s.n_items)) break;
+      }
+      while (alive && weighed < item) weigh_values(weighed++);
+      // what was issued has to be over before shared memory and TMEM go: a commit of its own, waited for whatever happened
+      tc_commit(bar_drain);
+    }
+    __syncwarp();
+    mbar_wait(bar_drain, 0, never);
+    __syncwarp();
+  } else {
+    // ===================== softmax: group g takes the tiles g, g + GROUPS, ... =====================
+    const int group = warp >> 2, quarter = warp & 3, tid = threadIdx.x & 127;         // tid: token of the tile (S), lane of O
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    const uint32_t t_s = tmem + lanes + group * C::S_COLS, t_o = tmem + lanes + GROUPS * C::S_COLS + group * C::P_COLS;
+    const uint32_t p_at = sb + C::O_P + group * C::P_BYTES;
+    float* red = reinterpret_cast<float*>(sm + C::O_RED) + group * 8 * R;             // [2][4][R]
+    float* stat = reinterpret_cast<float*>(sm + C::O_STAT);                           // [group][R] A, M; [group][4][R]
+    float* stat_a = stat + group * R;
+    float* stat_m = stat + GROUPS * R + group * R;
+    float* stat_l = stat + 2 * GROUPS * R + group * 4 * R;
+    float* join = reinterpret_cast<float*>(sm + C::O_JOIN);
+    float* table = reinterpret_cast<float*>(sm + C::O_TABLE) + warp * R * 8;
+    const int dim = D == 64 ? 16 * quarter + (lane & 15) : tid;                       // of O; with M = 64 the dimensions are lanes 0 .. 15 of each quarter
+    const bool has_dim = D != 64 || lane < 16;
+    int item = 0, mine = 0;                                                           // the CTA's tiles before this segment; the group's own so far
+    for (int n = 0;; ++n) {
+      const Seg s = segment(at);
+      const int buf = n & 1, n_tiles = s.last - s.first;
+      float o[R], l[R], top_a = -INFINITY, top_m = -INFINITY;                          // lane r: what row r's sums are relative to
+#pragma unroll
+      for (int r = 0; r < R; ++r) o[r] = l[r] = 0.0f;
+      if (!mbar_wait(bar_qfull + 8 * buf, (uint32_t)((n >> 1) & 1), abort_flag)) fail(7);
+      __syncwarp();
+      int see_all = 0x7FFFFFFF;                                                       // keys that every row sees
+      for (int r = 0; r < R; ++r)
+        if (r < a.tq * a.Gc) see_all = min(see_all, row_keys[buf * R + r]);
+      for (int i = (group - item % GROUPS + GROUPS) % GROUPS; i < n_tiles; i += GROUPS, ++mine) {
+        const int stage = (item + i) % ST, tok = (s.first + i) * TK + tid;
+        const bool edge = (s.first + i + 1) * TK > see_all;
+        if (!mbar_wait(bar_sfull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(8);
+        __syncwarp();
+        tc_fence_after();
+        // ---- this token's scales; those of the tile's largest page.  (the values' barrier: their scales are in place)
+        if (!mbar_wait(bar_vfull + 8 * stage, (uint32_t)(((item + i) / ST) & 1), abort_flag)) fail(9);
+        __syncwarp();
+        const int boxes = TK >> a.c.page_log2, live = min(boxes, ((s.keys - (s.first + i) * TK - 1) >> a.c.page_log2) + 1);
+        float sv_top = 0.0f;
+        for (int x = 0; x < live; ++x) {
+          const float v = meta_v[stage * 8 + x];
+          sv_top = v < INFINITY ? fmaxf(sv_top, v) : sv_top;
+        }
+        const int box = tid >> a.c.page_log2;
+        const bool some = box < live;
+        const float sk = some ? meta_k[stage * 8 + box] : 0.0f, sv = some ? meta_v[stage * 8 + box] : 0.0f;
+        const bool bad_v = !(sv >= 0.0f && sv < INFINITY);
+        const float lg_top = sv_top > 0.0f ? log2f(sv_top) : 0.0f;
+        const float lg = !bad_v && sv > 0.0f ? log2f(sv) : -INFINITY, lg_max = fmaxf(lg, lg_top - 60.0f);
+        float v[R];
+        uint32_t seen = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+          uint32_t x[24];
+          tc_ld8(t_s + 24 * c, x);
+          tc_ld8(t_s + 24 * c + 8, x + 8);
+          tc_ld8(t_s + 24 * c + 16, x + 16);
+          tc_wait_ld();
+          float w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 8 * c + j;
+            const float2 f = row_scale[buf * R + r];
+            const float dot = __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
+            v[r] = dot * (sk * f.x) * f.y;
+            if (edge && tok >= row_keys[buf * R + r]) v[r] = -INFINITY;
+            else seen |= 1u << r;
+            w[j] = v[r] + lg_max;
+          }
+          const float t = reduce8(w, lane, [](float x, float y) { return fmaxf(x, y); });
+          if ((lane & 3) == 0) red[((mine & 1) * 4 + quarter) * R + 8 * c + reduce8_row(lane)] = t;
+        }
+        if (bad_v && seen) atomicOr(broken + group, seen);
+        group_meet(group);
+        if (lane < R) {                                                               // what all threads want to know of row `lane`
+          float top = -INFINITY;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) top = fmaxf(top, red[((mine & 1) * 4 + q) * R + lane]);
+          const float mn = fmaxf(top_m, top - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
+          const float an = fmaxf(top_a, top), as = an == -INFINITY ? 0.0f : an;
+          float4* to = reinterpret_cast<float4*>(table + lane * 8);
+          to[0] = make_float4(ms, top == -INFINITY ? 0.0f : top, ex2(top_m - ms), 0.0f);
+          to[1] = make_float4(ex2(top_a - as), top == -INFINITY ? 0.0f : ex2(top - as), 0.0f, 0.0f);   // O so far, the tile's O
+          top_m = mn, top_a = an;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 8 * c + j;
+            const float4 f = *reinterpret_cast<const float4*>(table + r * 8);
+            l[r] = __fmaf_rn(l[r], f.z, ex2(v[r] - f.x));
+            const uint32_t u = __float2uint_rn(ex2(v[r] + lg - f.y) * W_ONE);
+            const uint32_t to = p_at + (24 * c + j) * TK + (tid ^ (j << 4));
+            sts8(to, u);
+            sts8(to + 8 * TK, u >> 8);
+            sts8(to + 16 * TK, u >> 16);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_before();
+        mbar_arrive(bar_pfull + 8 * group);
+        if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(10);
+        __syncwarp();
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+          uint32_t x[24];
+          tc_ld8(t_o + 24 * c, x);
+          tc_ld8(t_o + 24 * c + 8, x + 8);
+          tc_ld8(t_o + 24 * c + 16, x + 16);
+          tc_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 8 * c + j;
+            const float2 f = *reinterpret_cast<const float2*>(table + r * 8 + 4);
+            o[r] = o[r] * f.x + f.y * __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
+          }
+        }
+      }
+      item += n_tiles;
+
+      // ---- the groups' parts together
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = l[8 * c + j];
+        const float t = reduce8(w, lane, [](float x, float y) { return x + y; });
+        if ((lane & 3) == 0) stat_l[quarter * R + 8 * c + reduce8_row(lane)] = t;
+      }
+      if (quarter == 0 && lane < R) stat_a[lane] = top_a, stat_m[lane] = top_m;
+      threads_meet<SOFT>();
+      const bool whole = s.first == 0 && s.n_items == at.tiles;
+      float* part = a.parts + ((long long)blockIdx.x * 2 + (s.first > 0 ? 0 : 1)) * C::PART_FLOATS;
+      uint32_t lost = 0;
+      for (int g = 0; g < GROUPS; ++g) lost |= broken[g];
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        if (has_dim) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = 8 * c + j;
+            float top = -INFINITY;
+            for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, stat[g * R + r]);
+            join[(group * 8 + j) * D + dim] = stat_a[r] == -INFINITY ? 0.0f : o[r] * ex2(stat_a[r] - top) * (1.0f / W_ONE);
+          }
+        }
+        threads_meet<SOFT>();
+        for (int x = threadIdx.x; x < 8 * (D / 4); x += SOFT) {
+          const int j = x / (D / 4), d = x % (D / 4) * 4, r = 8 * c + j;
+          float ta = -INFINITY, tm = -INFINITY, sum_l = 0.0f;
+          float4 sum = make_float4(0, 0, 0, 0);
+          for (int g = 0; g < GROUPS; ++g) ta = fmaxf(ta, stat[g * R + r]), tm = fmaxf(tm, stat[GROUPS * R + g * R + r]);
+          for (int g = 0; g < GROUPS; ++g) {
+            const float4 v = *reinterpret_cast<const float4*>(join + (g * 8 + j) * D + d);
+            sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+            const float* q = stat + 2 * GROUPS * R + g * 4 * R + r;
+            const float lg = q[0] + q[R] + q[2 * R] + q[3 * R];
+            sum_l += rebase(stat[GROUPS * R + g * R + r], lg, tm) * lg;
+          }
+          if ((lost >> r) & 1u) sum.x = sum.y = sum.z = sum.w = __uint_as_float(0x7FC00000u);
+          if (whole) {
+            const int i = s.qt * a.tq + r / a.Gc, hq = s.chunk * a.Gc + r % a.Gc;
+            if (r < a.tq * a.Gc && i < at.n && hq < a.G) attn_store<D>(a, (long long)(at.row0 + i) * a.c.heads * a.G + s.h * a.G + hq, d, sum, sum_l, ta, tm);
+          } else {
+            __stcg(reinterpret_cast<float4*>(part + r * D + d), sum);
+            if (d == 0) {
+              __stcg(part + R * D + r, ta);
+              __stcg(part + R * D + R + r, tm);
+              __stcg(part + R * D + 2 * R + r, sum_l);
+            }
+          }
+        }
+        threads_meet<SOFT>();
+      }
+      if (!whole) attn_combine<D, R, SOFT, C::PART_FLOATS>(a, at, s.qt, s.h, s.chunk, begin + (end - begin - at.left) - s.first, per, misc + 7);
+      if (threadIdx.x == 0) {
+        for (int g = 0; g < GROUPS; ++g) broken[g] = 0;
+        mbar_arrive(bar_qempty + 8 * buf);                                            // queries, factors and statistics of the unit are done with
+      }
+      threads_meet<SOFT>();
+      if (!walk_advance(a, TK, at, s.n_items)) break;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == C::W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::TMEM_COLS) : "memory");
+}
+
+template <int D, int R>
+int launch_as(AttnArgs& a, cudaStream_t st) {
+  using C = FewCfg<D, R>;
+  static_assert(C::SMEM_BYTES <= 232448, "shared memory of a CTA");
+  a.Gc = a.G < R ? a.G : R;
+  a.chunks = (a.G + a.Gc - 1) / a.Gc;
+  a.tq = R / a.Gc;
+  CUtensorMap map_k, map_v;
+  RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, a.c.page));
+  RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page));
+  static std::atomic<uint64_t> allowed{0};
+  RAZER_TRY(allow_smem((const void*)attn_kv8_few_kernel<D, R>, C::SMEM_BYTES, allowed));
+  return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R>, sm_count(), C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
+}
+
+}  // namespace
+
+size_t attn_few_part_floats(int D) { return D == 64 ? FewCfg<64, 32>::PART_FLOATS : FewCfg<128, 32>::PART_FLOATS; }
+
+int launch_attn_few(AttnArgs& a, int rows, cudaStream_t st) {
+  if (a.c.D == 64) return rows <= 8 ? launch_as<64, 8>(a, st) : rows <= 16 ? launch_as<64, 16>(a, st) : launch_as<64, 32>(a, st);
+  return rows <= 8 ? launch_as<128, 8>(a, st) : rows <= 16 ? launch_as<128, 16>(a, st) : launch_as<128, 32>(a, st);
+}
+
+}  // namespace razer

@@ -2,9 +2,11 @@
 
 Bar of the attention.  Exact result o = sum p_j v_j / sum p_j.  What is rounded: the query row to f16 with a scale of its own (exact for bf16
 but for values below 2^-28 of the row's largest), scores and their exponents in FP32 (a score of magnitude S is off by at most (D + 4) 2^-24 S_abs with
-S_abs = scale * ks * sum_d |q_d k_d|; the tensor core's truncated additions are counted as 2^-23 each, and the exponential as 2^-21), probabilities to
-f16 (2^-11 of each, or 2^-39 of the largest), sums in FP32, the result to bf16 (2^-8).  So with A = sum p_j |v_j| / sum p_j and E = 2^-23 (D + 4) max S_abs + 2^-21:
-   |out - o| <= 2^-8 |o| + (2^-11 + 2 E + 2^-20) A + 2^-38 max |v|
+S_abs = scale * ks * sum_d |q_d k_d|; the tensor core's truncated additions are counted as 2^-23 each, and the exponential as 2^-21), weights
+p_j vs_j either to f16 (2^-11 of each, or 2^-39 of the largest) or to 24 bits of the largest among 128 tokens (2^-25 of that), sums in FP32, the result to bf16 (2^-8).
+A weight that is off by 2^-25 W, W = max p_j vs_j, moves the numerator by at most 2^-25 W |code| <= 2^-25 W 127, and n keys by n times that.  So
+with A = sum p_j |v_j| / sum p_j and E = 2^-23 (D + 4) max S_abs + 2^-21:
+   |out - o| <= 2^-8 |o| + (2^-11 + 2 E + 2^-20) A + 2^-38 max |v| + 2^-25 127 n W / sum p_j
    |lse - exact| <= E + 2^-22 |exact| + 2^-21
 """
 import math
@@ -208,7 +210,9 @@ def check_attn(b, s, q, scale=None, workspace=None):
                 size = p @ v.abs()
                 top = v.abs().max() if v.numel() else 0.0
                 e = 2.0 ** -23 * (s.D + 4) * room + 2.0 ** -21
-                bar = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * e[:, None] + 2.0 ** -20) * size + 2.0 ** -38 * top
+                sv = s.vs[s.table[i, :-(-s.total[i] // s.page)].long(), h].double().repeat_interleave(s.page)[:max(s.total[i], 0)]
+                most = (p * sv).max(dim=1, keepdim=True).values * 127 * (limit[:, None] + 1).clamp(min=0) if p.shape[1] else 0.0
+                bar = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * e[:, None] + 2.0 ** -20) * size + 2.0 ** -38 * top + 2.0 ** -25 * most
                 off = (out[rows, h * G + gq] - want).abs()
                 assert (off <= bar).all(), (i, h, gq, float((off / bar.clamp(min=1e-300)).max()))
                 worst = max(worst, float((off / bar.clamp(min=1e-300)).max()))
