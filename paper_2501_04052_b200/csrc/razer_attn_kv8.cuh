@@ -129,9 +129,10 @@ __device__ __forceinline__ void attn_store(const AttnArgs& a, long long row, int
 template <int D, int R, int THREADS, int PART_FLOATS>
 __device__ __forceinline__ void attn_combine(const AttnArgs& a, const Walk& at, int qt, int h, int chunk, long long unit_begin, long long per, int* flag) {
   const int c_first = (int)(unit_begin / per), c_last = (int)((unit_begin + at.tiles - 1) / per);
-  __threadfence();
   threads_meet<THREADS>();
   if (threadIdx.x == 0) {
+    // release: the part's stores (ordered before this by the meeting) become visible with the count; acquire: so do the others' to what follows the
+    // next meeting
     uint32_t seen;
     asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.counters + c_first) : "memory");
     *flag = seen == (uint32_t)(c_last - c_first);
@@ -139,28 +140,41 @@ __device__ __forceinline__ void attn_combine(const AttnArgs& a, const Walk& at, 
   }
   threads_meet<THREADS>();
   if (!*flag) return;
-  __threadfence();
   for (int x = threadIdx.x; x < R * (D / 4); x += THREADS) {
     const int r = x / (D / 4), d = x % (D / 4) * 4;
     const int i = qt * a.tq + r / a.Gc, hq = chunk * a.Gc + r % a.Gc;
     if (!(r < a.tq * a.Gc && i < at.n && hq < a.G)) continue;
     float ta = -INFINITY, tm = -INFINITY, sum_l = 0.0f;
     float4 sum = make_float4(0, 0, 0, 0);
-    for (int c = c_first; c <= c_last; ++c) {
-      const float* p = a.parts + ((long long)c * 2 + (c == c_first)) * PART_FLOATS + R * D + r;
-      ta = fmaxf(ta, __ldcg(p));
-      tm = fmaxf(tm, __ldcg(p + R));
-    }
-    for (int c = c_first; c <= c_last; ++c) {
-      const float* p = a.parts + ((long long)c * 2 + (c == c_first)) * PART_FLOATS;
-      const float ac = __ldcg(p + R * D + r), mc = __ldcg(p + R * D + R + r), lc = __ldcg(p + R * D + 2 * R + r);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
-      const float f = ac == -INFINITY ? 0.0f : ex2(ac - ta);
-      sum_l += rebase(mc, lc, tm) * lc;
-      sum.x += f * v.x;
-      sum.y += f * v.y;
-      sum.z += f * v.z;
-      sum.w += f * v.w;
+    // eight parts in flight; what was added up so far moves to the larger maximum
+    constexpr int U = 8;
+    for (int c0 = c_first; c0 <= c_last; c0 += U) {
+      float ac[U], mc[U], lc[U];
+      float4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = min(c0 + u, c_last);
+        const float* p = a.parts + ((long long)c * 2 + (c == c_first)) * PART_FLOATS;
+        ac[u] = __ldcg(p + R * D + r), mc[u] = __ldcg(p + R * D + R + r), lc[u] = __ldcg(p + R * D + 2 * R + r);
+        v[u] = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
+      }
+      float na = ta, nm = tm;
+#pragma unroll
+      for (int u = 0; u < U; ++u) na = fmaxf(na, ac[u]), nm = fmaxf(nm, mc[u]);
+      const float f0 = ta == -INFINITY ? 0.0f : ex2(ta - na);
+      sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
+      sum_l *= rebase(tm, sum_l, nm);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (c0 + u > c_last) break;
+        const float f = ac[u] == -INFINITY ? 0.0f : ex2(ac[u] - na);
+        sum_l += rebase(mc[u], lc[u], nm) * lc[u];
+        sum.x += f * v[u].x;
+        sum.y += f * v[u].y;
+        sum.z += f * v[u].z;
+        sum.w += f * v[u].w;
+      }
+      ta = na, tm = nm;
     }
     attn_store<D>(a, (long long)(at.row0 + i) * a.c.heads * a.G + h * a.G + hq, d, sum, sum_l, ta, tm);
   }

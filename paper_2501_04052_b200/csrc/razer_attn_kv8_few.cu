@@ -32,6 +32,7 @@ struct FewCfg {
   static constexpr int NS = R_ == 8 ? 32 : 3 * R_, NP = NS;                                // columns of S and of O
   static constexpr int Q_BYTES = NS * D, P_BYTES = NP * TK;
   static constexpr int STAGES = (D_ == 64 ? 2 : 1) * (R_ <= 16 ? 6 : 5);
+  static constexpr int TABLES = CHUNKS == 1 ? 2 : 1;
   static constexpr int O_RING = 0;
   static constexpr int O_Q = STAGES * STAGE_BYTES;                     // two buffers, [column][D]
   static constexpr int O_P = (O_Q + 2 * Q_BYTES + 1023) / 1024 * 1024; // [group][column][128]
@@ -40,10 +41,10 @@ struct FewCfg {
   static constexpr int O_JOIN = JOIN_ON_P ? O_P : O_P + GROUPS * P_BYTES;
   static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][2][4 warps][R]
   static constexpr int O_STAT = O_RED + GROUPS * 8 * R * 4;            // [group][R] A, M; [group][4][R] sums
-  static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][R][8] what a tile means for each row
-  static constexpr int O_ROW = O_TABLE + 4 * GROUPS * R * 32;          // [2][R] score factor in two parts; [2][R] keys
-  static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] key scales, then value scales
-  static constexpr int O_BAR = O_META + STAGES * 64;
+  static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][TABLES][R][8] what a tile means for each row
+  static constexpr int O_ROW = O_TABLE + 4 * GROUPS * TABLES * R * 32; // [2][R] score factor in two parts; [2][R] keys
+  static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] {key scale, log2 of the value scale}, [STAGES] the largest of the latter
+  static constexpr int O_BAR = (O_META + STAGES * 68 + 7) / 8 * 8;
   static constexpr int N_BAR = 3 * STAGES + 3 * GROUPS + 5;
   static constexpr int O_MISC = O_BAR + 8 * N_BAR;                     // words: abort, never set, share (4 words), TMEM, last, broken values by group, sums
   static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
@@ -99,8 +100,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
   volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(misc);
   volatile uint32_t* never = reinterpret_cast<uint32_t*>(misc + 1);
   uint32_t* broken = reinterpret_cast<uint32_t*>(misc + 8);              // [group] rows that saw a value scale that is none
-  float* meta_k = reinterpret_cast<float*>(sm + C::O_META);
-  float* meta_v = meta_k + 8 * ST;
+  float2* meta = reinterpret_cast<float2*>(sm + C::O_META);
+  float* meta_top = reinterpret_cast<float*>(meta + 8 * ST);
   float2* row_scale = reinterpret_cast<float2*>(sm + C::O_ROW);           // [2][R]
   int* row_keys = reinterpret_cast<int*>(row_scale + 2 * R);              // [2][R]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     do {
       const Seg g = segment(at);
       int have = -64, id = -1, id_next = -1;                     // first of the 32 blocks that the lanes hold; the lane's page of these and of the next 32
-      float ks = 0, vs = 0;                                      // the values' warp brings both kinds of scales
+      float ks = 0, lg = 0;                                      // the values' warp brings the scales: keys', and log2 of the values'
       auto page_of = [&](int block) { return ((long long)block << a.c.page_log2) < g.keys ? kv8_page(a.c, a.s, at.b, block) : -1; };
       for (int t = g.first; t < g.last; ++t, ++item) {
         const int block0 = t * boxes, stage = item % ST;
@@ -179,10 +180,13 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           id = block0 == have + 32 ? id_next : page_of(block0 + lane);
           have = block0;
           id_next = page_of(have + 32 + lane);
-          ks = vs = __uint_as_float(0x7FC00000u);
-          if (value && id >= 0) {
-            ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + g.h);
-            vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
+          if (value) {
+            float vs = ks = __uint_as_float(0x7FC00000u);
+            if (id >= 0) {
+              ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + g.h);
+              vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
+            }
+            lg = vs >= 0.0f && vs < INFINITY ? log2f(vs) : __uint_as_float(0x7FC00000u);   // -infinity for 0
           }
         }
         if (item >= ST && !mbar_wait(bar_empty + 8 * stage, (uint32_t)((item / ST) & 1) ^ 1u, abort_flag)) {
@@ -195,8 +199,13 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         const int live = min(boxes, ((g.keys - t * TK - 1) >> a.c.page_log2) + 1);
         const int page = __shfl_sync(0xFFFFFFFFu, id, (block0 - have + lane) & 31);
         if (value) {
-          const float k1 = __shfl_sync(0xFFFFFFFFu, ks, (block0 - have + lane) & 31), v1 = __shfl_sync(0xFFFFFFFFu, vs, (block0 - have + lane) & 31);
-          if (lane < boxes) meta_k[stage * 8 + lane] = k1, meta_v[stage * 8 + lane] = v1;
+          float k1 = __shfl_sync(0xFFFFFFFFu, ks, (block0 - have + lane) & 31), v1 = __shfl_sync(0xFFFFFFFFu, lg, (block0 - have + lane) & 31);
+          if (lane >= live) k1 = 0.0f, v1 = -INFINITY;           // no token that anyone sees
+          float most = v1;
+          for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+          if (!(most > -INFINITY)) most = 0.0f;                  // all of them 0 or broken
+          if (lane < 8) meta[stage * 8 + lane] = make_float2(k1, v1);
+          if (lane == 0) meta_top[stage] = most;
           __syncwarp();
         }
         if (lane == 0) mbar_expect_tx(bar, (uint32_t)((live << a.c.page_log2) * D));
@@ -334,7 +343,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     float* stat_m = stat + GROUPS * R + group * R;
     float* stat_l = stat + 2 * GROUPS * R + group * 4 * R;
     float* join = reinterpret_cast<float*>(sm + C::O_JOIN);
-    float* table = reinterpret_cast<float*>(sm + C::O_TABLE) + warp * R * 8;
+    float* table = reinterpret_cast<float*>(sm + C::O_TABLE) + warp * C::TABLES * R * 8;
     const int dim = D == 64 ? 16 * quarter + (lane & 15) : tid;                       // of O; with M = 64 the dimensions are lanes 0 .. 15 of each quarter
     const bool has_dim = D != 64 || lane < 16;
     int item = 0, mine = 0;                                                           // the CTA's tiles before this segment; the group's own so far
@@ -349,99 +358,121 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       int see_all = 0x7FFFFFFF;                                                       // keys that every row sees
       for (int r = 0; r < R; ++r)
         if (r < a.tq * a.Gc) see_all = min(see_all, row_keys[buf * R + r]);
+      // O of the group's last tile into the running sums; the registers come first, so that the next product may begin
+      uint32_t x_o[CHUNKS == 1 ? 24 : 1];
+      auto take = [&](int c, const uint32_t (&x)[24], const float* t) {
+        float2 f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float2*>(t + (8 * c + j) * 8 + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[8 * c + j] = o[8 * c + j] * f[j].x + f[j].y * __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
+      };
+      auto load24 = [&](uint32_t t, uint32_t (&x)[24]) {
+        tc_ld8(t, x);
+        tc_ld8(t + 8, x + 8);
+        tc_ld8(t + 16, x + 16);
+        tc_wait_ld();
+      };
+      bool pending = false;                                                           // the last tile's product with the values is not in yet
+      auto take_all = [&]() {
+        if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)((mine - 1) & 1), abort_flag)) fail(10);
+        __syncwarp();
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+          uint32_t x[24];
+          load24(t_o + 24 * c, x);
+          take(c, x, table + ((mine - 1) % C::TABLES) * R * 8);
+        }
+        pending = false;
+      };
       for (int i = (group - item % GROUPS + GROUPS) % GROUPS; i < n_tiles; i += GROUPS, ++mine) {
         const int stage = (item + i) % ST, tok = (s.first + i) * TK + tid;
         const bool edge = (s.first + i + 1) * TK > see_all;
+        float* tab = table + (mine % C::TABLES) * R * 8;
+        float* red_now = red + (mine & 1) * 4 * R;
+        // the values' barrier first: their warp has the scales
+        if (!mbar_wait(bar_vfull + 8 * stage, (uint32_t)(((item + i) / ST) & 1), abort_flag)) fail(9);
+        const float2 sc = meta[stage * 8 + (tid >> a.c.page_log2)];
+        const float lg_top = meta_top[stage], lg = sc.y, lg_max = fmaxf(lg, lg_top - 60.0f);   // (a NaN becomes the floor)
         if (!mbar_wait(bar_sfull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(8);
         __syncwarp();
         tc_fence_after();
-        // ---- this token's scales; those of the tile's largest page.  (the values' barrier: their scales are in place)
-        if (!mbar_wait(bar_vfull + 8 * stage, (uint32_t)(((item + i) / ST) & 1), abort_flag)) fail(9);
-        __syncwarp();
-        const int boxes = TK >> a.c.page_log2, live = min(boxes, ((s.keys - (s.first + i) * TK - 1) >> a.c.page_log2) + 1);
-        float sv_top = 0.0f;
-        for (int x = 0; x < live; ++x) {
-          const float v = meta_v[stage * 8 + x];
-          sv_top = v < INFINITY ? fmaxf(sv_top, v) : sv_top;
-        }
-        const int box = tid >> a.c.page_log2;
-        const bool some = box < live;
-        const float sk = some ? meta_k[stage * 8 + box] : 0.0f, sv = some ? meta_v[stage * 8 + box] : 0.0f;
-        const bool bad_v = !(sv >= 0.0f && sv < INFINITY);
-        const float lg_top = sv_top > 0.0f ? log2f(sv_top) : 0.0f;
-        const float lg = !bad_v && sv > 0.0f ? log2f(sv) : -INFINITY, lg_max = fmaxf(lg, lg_top - 60.0f);
         float v[R];
         uint32_t seen = 0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
+          float2 f[8];
+          int keys[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            f[j] = row_scale[buf * R + 8 * c + j];
+            keys[j] = edge ? row_keys[buf * R + 8 * c + j] : 0x7FFFFFFF;
+          }
           uint32_t x[24];
-          tc_ld8(t_s + 24 * c, x);
-          tc_ld8(t_s + 24 * c + 8, x + 8);
-          tc_ld8(t_s + 24 * c + 16, x + 16);
-          tc_wait_ld();
+          load24(t_s + 24 * c, x);
           float w[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int r = 8 * c + j;
-            const float2 f = row_scale[buf * R + r];
             const float dot = __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
-            v[r] = dot * (sk * f.x) * f.y;
-            if (edge && tok >= row_keys[buf * R + r]) v[r] = -INFINITY;
-            else seen |= 1u << r;
+            v[r] = tok < keys[j] ? dot * (sc.x * f[j].x) * f[j].y : -INFINITY;
+            seen |= tok < keys[j] ? 1u << r : 0u;
             w[j] = v[r] + lg_max;
           }
           const float t = reduce8(w, lane, [](float x, float y) { return fmaxf(x, y); });
-          if ((lane & 3) == 0) red[((mine & 1) * 4 + quarter) * R + 8 * c + reduce8_row(lane)] = t;
+          if ((lane & 3) == 0) red_now[quarter * R + 8 * c + reduce8_row(lane)] = t;
         }
-        if (bad_v && seen) atomicOr(broken + group, seen);
+        if (lg != lg && seen) atomicOr(broken + group, seen);                         // a value scale that is none
+        // The last tile's product has read its digits by then, and gives way to this one's once it is in registers: late for eight rows, here for more.
+        if (CHUNKS > 1 && pending) take_all();
         group_meet(group);
         if (lane < R) {                                                               // what all threads want to know of row `lane`
           float top = -INFINITY;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) top = fmaxf(top, red[((mine & 1) * 4 + q) * R + lane]);
+          for (int q = 0; q < 4; ++q) top = fmaxf(top, red_now[q * R + lane]);
           const float mn = fmaxf(top_m, top - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
           const float an = fmaxf(top_a, top), as = an == -INFINITY ? 0.0f : an;
-          float4* to = reinterpret_cast<float4*>(table + lane * 8);
+          float4* to = reinterpret_cast<float4*>(tab + lane * 8);
           to[0] = make_float4(ms, top == -INFINITY ? 0.0f : top, ex2(top_m - ms), 0.0f);
-          to[1] = make_float4(ex2(top_a - as), top == -INFINITY ? 0.0f : ex2(top - as), 0.0f, 0.0f);   // O so far, the tile's O
+          to[1] = make_float4(ex2(top_a - as), (top == -INFINITY ? 0.0f : ex2(top - as)), 0.0f, 0.0f);   // O so far, the tile's O
           top_m = mn, top_a = an;
         }
         __syncwarp();
+        const float lg_w = lg != lg ? -INFINITY : lg;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
+          float4 f[8];
+          uint32_t u[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float4*>(tab + (8 * c + j) * 8);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int r = 8 * c + j;
-            const float4 f = *reinterpret_cast<const float4*>(table + r * 8);
-            l[r] = __fmaf_rn(l[r], f.z, ex2(v[r] - f.x));
-            const uint32_t u = __float2uint_rn(ex2(v[r] + lg - f.y) * W_ONE);
+            l[r] = __fmaf_rn(l[r], f[j].z, ex2(v[r] - f[j].x));
+            u[j] = __float2uint_rn(ex2(v[r] + lg_w - f[j].y) * W_ONE);
+          }
+          if (CHUNKS == 1 && pending) {
+            if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)((mine - 1) & 1), abort_flag)) fail(10);
+            __syncwarp();
+            tc_fence_after();
+            load24(t_o, reinterpret_cast<uint32_t(&)[24]>(x_o));
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
             const uint32_t to = p_at + (24 * c + j) * TK + (tid ^ (j << 4));
-            sts8(to, u);
-            sts8(to + 8 * TK, u >> 8);
-            sts8(to + 16 * TK, u >> 16);
+            sts8(to, u[j]);
+            sts8(to + 8 * TK, u[j] >> 8);
+            sts8(to + 16 * TK, u[j] >> 16);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         mbar_arrive(bar_pfull + 8 * group);
-        if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(10);
-        __syncwarp();
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          uint32_t x[24];
-          tc_ld8(t_o + 24 * c, x);
-          tc_ld8(t_o + 24 * c + 8, x + 8);
-          tc_ld8(t_o + 24 * c + 16, x + 16);
-          tc_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = 8 * c + j;
-            const float2 f = *reinterpret_cast<const float2*>(table + r * 8 + 4);
-            o[r] = o[r] * f.x + f.y * __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
-          }
-        }
+        if (CHUNKS == 1 && pending) take(0, reinterpret_cast<uint32_t(&)[24]>(x_o), table + ((mine - 1) % C::TABLES) * R * 8);
+        pending = true;
       }
+      if (pending) take_all();
       item += n_tiles;
 
       // ---- the groups' parts together
