@@ -124,59 +124,72 @@ __device__ __forceinline__ void attn_store(const AttnArgs& a, long long row, int
   if (d == 0 && a.lse) a.lse[row] = none ? -INFINITY : (tm + log2f(sum_l)) * LN2;
 }
 
+constexpr int ATTN_CTAS = 152;                            // CTAs of a launch at most
+
 // The CTA has left its part of a unit that others share ([R][D] sums, then [R] ta, tm, sum_l; a CTA's first unit in its slot 0, its last in
-// slot 1); the last of them to come here finishes it.  THREADS threads (threads_meet); `flag`: a word of shared memory.
+// slot 1); the last of them to come here finishes it.  THREADS threads (threads_meet); `flag`: a word of shared memory, `scratch`: (ATTN_CTAS + 3) R floats.
+// Code that runs once is held short: what a CTA does not have in its instruction cache costs it some 15 cycles an instruction (16 parts put together by
+// code unrolled eight times 8900 cycles).
 template <int D, int R, int THREADS, int PART_FLOATS>
-__device__ __forceinline__ void attn_combine(const AttnArgs& a, const Walk& at, int qt, int h, int chunk, long long unit_begin, long long per, int* flag) {
-  const int c_first = (int)(unit_begin / per), c_last = (int)((unit_begin + at.tiles - 1) / per);
+__device__ __forceinline__ void attn_combine(const AttnArgs& a, const Walk& at, int qt, int h, int chunk, long long unit_begin, long long per, int* flag, float* scratch) {
+  const int c_first = (int)(unit_begin / per), parts = (int)((unit_begin + at.tiles - 1) / per) - c_first + 1;
   threads_meet<THREADS>();
   if (threadIdx.x == 0) {
     // release: the part's stores (ordered before this by the meeting) become visible with the count; acquire: so do the others' to what follows the
     // next meeting
     uint32_t seen;
     asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.counters + c_first) : "memory");
-    *flag = seen == (uint32_t)(c_last - c_first);
+    *flag = seen == (uint32_t)(parts - 1);
     if (*flag) a.counters[c_first] = 0;                  // ready for the next call
   }
   threads_meet<THREADS>();
   if (!*flag) return;
+  const float* p0 = a.parts + ((long long)c_first * 2 + 1) * PART_FLOATS;              // the first CTA's; the others' lie 2 PART_FLOATS apart from the next slot 0 on
+  auto part = [&](int c) { return p0 + (c > 0 ? (long long)(2 * c - 1) * PART_FLOATS : 0); };
+  const int lane = threadIdx.x & 31;
+  float* rows = scratch + ATTN_CTAS * R;                 // [R] ta, tm, sum_l
+#pragma unroll 1
+  for (int r = threadIdx.x >> 5; r < R; r += THREADS / 32) {
+    float ta = -INFINITY, tm = -INFINITY, sum_l = 0.0f;
+#pragma unroll 1
+    for (int c = lane; c < parts; c += 32) {
+      const float* p = part(c) + R * D + r;
+      const float ac = __ldcg(p), mc = __ldcg(p + R), lc = __ldcg(p + 2 * R), nm = fmaxf(tm, mc);
+      scratch[c * R + r] = ac;
+      ta = fmaxf(ta, ac);
+      sum_l = rebase(tm, sum_l, nm) * sum_l + rebase(mc, lc, nm) * lc;
+      tm = nm;
+    }
+    float top = tm;
+    for (int x = 16; x; x >>= 1) {
+      ta = fmaxf(ta, __shfl_xor_sync(0xFFFFFFFFu, ta, x));
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+    }
+    sum_l *= rebase(tm, sum_l, top);
+    for (int x = 16; x; x >>= 1) sum_l += __shfl_xor_sync(0xFFFFFFFFu, sum_l, x);
+    for (int c = lane; c < parts; c += 32) {
+      const float ac = scratch[c * R + r];
+      scratch[c * R + r] = ac == -INFINITY ? 0.0f : ex2(ac - ta);
+    }
+    if (lane == 0) rows[r] = ta, rows[R + r] = top, rows[2 * R + r] = sum_l;
+  }
+  threads_meet<THREADS>();
+#pragma unroll 1
   for (int x = threadIdx.x; x < R * (D / 4); x += THREADS) {
     const int r = x / (D / 4), d = x % (D / 4) * 4;
     const int i = qt * a.tq + r / a.Gc, hq = chunk * a.Gc + r % a.Gc;
     if (!(r < a.tq * a.Gc && i < at.n && hq < a.G)) continue;
-    float ta = -INFINITY, tm = -INFINITY, sum_l = 0.0f;
     float4 sum = make_float4(0, 0, 0, 0);
-    // eight parts in flight; what was added up so far moves to the larger maximum
-    constexpr int U = 8;
-    for (int c0 = c_first; c0 <= c_last; c0 += U) {
-      float ac[U], mc[U], lc[U];
-      float4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = min(c0 + u, c_last);
-        const float* p = a.parts + ((long long)c * 2 + (c == c_first)) * PART_FLOATS;
-        ac[u] = __ldcg(p + R * D + r), mc[u] = __ldcg(p + R * D + R + r), lc[u] = __ldcg(p + R * D + 2 * R + r);
-        v[u] = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
-      }
-      float na = ta, nm = tm;
-#pragma unroll
-      for (int u = 0; u < U; ++u) na = fmaxf(na, ac[u]), nm = fmaxf(nm, mc[u]);
-      const float f0 = ta == -INFINITY ? 0.0f : ex2(ta - na);
-      sum.x *= f0, sum.y *= f0, sum.z *= f0, sum.w *= f0;
-      sum_l *= rebase(tm, sum_l, nm);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (c0 + u > c_last) break;
-        const float f = ac[u] == -INFINITY ? 0.0f : ex2(ac[u] - na);
-        sum_l += rebase(mc[u], lc[u], nm) * lc[u];
-        sum.x += f * v[u].x;
-        sum.y += f * v[u].y;
-        sum.z += f * v[u].z;
-        sum.w += f * v[u].w;
-      }
-      ta = na, tm = nm;
+#pragma unroll 4
+    for (int c = 0; c < parts; ++c) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(part(c) + r * D + d));
+      const float f = scratch[c * R + r];
+      sum.x += f * v.x;
+      sum.y += f * v.y;
+      sum.z += f * v.z;
+      sum.w += f * v.w;
     }
-    attn_store<D>(a, (long long)(at.row0 + i) * a.c.heads * a.G + h * a.G + hq, d, sum, sum_l, ta, tm);
+    attn_store<D>(a, (long long)(at.row0 + i) * a.c.heads * a.G + h * a.G + hq, d, sum, rows[2 * R + r], rows[r], rows[R + r]);
   }
 }
 

@@ -36,7 +36,7 @@ struct FewCfg {
   static constexpr int O_RING = 0;
   static constexpr int O_Q = STAGES * STAGE_BYTES;                     // two buffers, [column][D]
   static constexpr int O_P = (O_Q + 2 * Q_BYTES + 1023) / 1024 * 1024; // [group][column][128]
-  static constexpr int JOIN_BYTES = GROUPS * 8 * D * 4;                // [group][8 rows][D] floats, over the digits where they have the room:
+  static constexpr int JOIN_BYTES = GROUPS * 32 * D > (ATTN_CTAS + 3) * R * 4 ? GROUPS * 32 * D : (ATTN_CTAS + 3) * R * 4;   // [group][8 rows][D] floats, then attn_combine's; over the digits where they have the room:
   static constexpr bool JOIN_ON_P = JOIN_BYTES <= GROUPS * P_BYTES;    // at a unit's end they have been read
   static constexpr int O_JOIN = JOIN_ON_P ? O_P : O_P + GROUPS * P_BYTES;
   static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][2][4 warps][R]
@@ -171,23 +171,37 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     bool alive = true;
     do {
       const Seg g = segment(at);
-      int have = -64, id = -1, id_next = -1;                     // first of the 32 blocks that the lanes hold; the lane's page of these and of the next 32
-      float ks = 0, lg = 0;                                      // the values' warp brings the scales: keys', and log2 of the values'
+      // The lanes hold 32 blocks from `have` on: pages and (values' warp) scales, the pages of the next 32, and the scales of those on their way
+      int have = (g.first * boxes) & ~31, id, id_next;
+      float ks = 0, lg = 0, ks_next = 0, vs_next = 0;            // key scale; log2 of the value scale; both of the next 32
       auto page_of = [&](int block) { return ((long long)block << a.c.page_log2) < g.keys ? kv8_page(a.c, a.s, at.b, block) : -1; };
+      auto ask = [&]() {
+        ks_next = vs_next = __uint_as_float(0x7FC00000u);
+        if (value && id_next >= 0) {
+          ks_next = __ldg(a.c.k_scales + (long long)id_next * a.c.heads + g.h);
+          vs_next = __ldg(a.c.v_scales + (long long)id_next * a.c.heads + g.h);
+        }
+      };
+      auto step = [&]() {
+        id = id_next;
+        ks = ks_next;
+        if (value) lg = vs_next >= 0.0f && vs_next < INFINITY ? log2f(vs_next) : __uint_as_float(0x7FC00000u);   // -infinity for 0
+      };
+      id_next = page_of(have + lane);
+      int id_after = page_of(have + 32 + lane);
+      ask();
+      step();
+      id_next = id_after;
+      ask();
+      id_after = page_of(have + 64 + lane);
       for (int t = g.first; t < g.last; ++t, ++item) {
         const int block0 = t * boxes, stage = item % ST;
-        if (block0 + boxes > have + 32) {
-          id = block0 == have + 32 ? id_next : page_of(block0 + lane);
-          have = block0;
-          id_next = page_of(have + 32 + lane);
-          if (value) {
-            float vs = ks = __uint_as_float(0x7FC00000u);
-            if (id >= 0) {
-              ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + g.h);
-              vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
-            }
-            lg = vs >= 0.0f && vs < INFINITY ? log2f(vs) : __uint_as_float(0x7FC00000u);   // -infinity for 0
-          }
+        if (block0 >= have + 32) {
+          have += 32;
+          step();
+          id_next = id_after;
+          ask();
+          id_after = page_of(have + 64 + lane);
         }
         if (item >= ST && !mbar_wait(bar_empty + 8 * stage, (uint32_t)((item / ST) & 1) ^ 1u, abort_flag)) {
           fail(1);
@@ -226,52 +240,52 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       if (n >= 2 && !mbar_wait(bar_qempty + 8 * buf, (uint32_t)((n >> 1) & 1) ^ 1u, abort_flag)) { fail(2); break; }
       __syncwarp();
       const bool over = kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
-      for (int c = 0; c < CHUNKS; ++c) {
-        uint32_t raw[8][D / 64];
-        bool real[8];
-        int keys[8];
+#pragma unroll 1
+      for (int c = 0; c < CHUNKS; ++c) {                          // eight rows at once, four lanes a row, D / 4 dimensions a lane
+        const int j = lane >> 2, part = lane & 3, r = 8 * c + j, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
+        const bool real = r < a.tq * a.Gc && i < at.n && hq < a.G;
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + part * (D / 32);
+        uint4 raw[D / 32];
+        uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int r = 8 * c + j, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
-          real[j] = r < a.tq * a.Gc && i < at.n && hq < a.G;
-          keys[j] = real[j] ? max(at.len - at.n + i + 1, 0) : 0;
-          const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + lane * (D / 64);
+        for (int k = 0; k < D / 32; ++k) raw[k] = real ? src[k] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-          for (int k = 0; k < D / 64; ++k) raw[j][k] = real[j] ? src[k] : 0u;
+        for (int k = 0; k < D / 32; ++k)
+          top = __vmaxu2(__vmaxu2(top, __vmaxu2(raw[k].x & 0x7FFF7FFFu, raw[k].y & 0x7FFF7FFFu)), __vmaxu2(raw[k].z & 0x7FFF7FFFu, raw[k].w & 0x7FFF7FFFu));
+        top = max(top >> 16, top & 0xFFFFu) << 16;
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const bool bad = top >= 0x7F800000u || over;
+        const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
+        const float up0 = power2((21 - e) / 2), up1 = power2(21 - e - (21 - e) / 2);
+        if (part == 0) {
+          row_scale[buf * R + r] = make_float2(bad ? __uint_as_float(0x7FC00000u) : a.scale * LOG2E * power2(e / 2), power2(e - e / 2 - 21));
+          row_keys[buf * R + r] = real ? max(at.len - at.n + i + 1, 0) : 0;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t top = 0;
+        for (int k = 0; k < D / 32; ++k) {
+          const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
-          for (int k = 0; k < D / 64; ++k) top = max(top, max((raw[j][k] & 0x7FFFu) << 16, raw[j][k] & 0x7FFF0000u));
-          top = __reduce_max_sync(0xFFFFFFFFu, top);
-          const bool bad = top >= 0x7F800000u || over;
-          const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
-          const float up0 = power2((21 - e) / 2), up1 = power2(21 - e - (21 - e) / 2);
-          const int row = buf * R + 8 * c + j;
-          if (lane == 0) {
-            row_scale[row] = make_float2(bad ? __uint_as_float(0x7FC00000u) : a.scale * LOG2E * power2(e / 2), power2(e - e / 2 - 21));
-            row_keys[row] = keys[j];
-          }
-          uint32_t digit[3] = {0, 0, 0};                          // D / 32 dimensions, a byte each
+          for (int b = 0; b < 2; ++b) {                           // four dimensions: a word of each digit
+            uint32_t digit[3] = {0, 0, 0};
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) {
-            const float x = __uint_as_float((k & 1) ? raw[j][k / 2] & 0xFFFF0000u : raw[j][k / 2] << 16);
-            int v = bad ? 0 : __float2int_rn(x * up0 * up1);
+            for (int m = 0; m < 4; ++m) {
+              const uint32_t pair = w[2 * b + (m >> 1)];
+              int v = bad ? 0 : __float2int_rn(__uint_as_float((m & 1) ? pair & 0xFFFF0000u : pair << 16) * up0 * up1);
+#pragma unroll
+              for (int q = 0; q < 3; ++q) {
+                const int lo = (int)(int8_t)v;
+                digit[q] |= (uint32_t)(lo & 255) << (8 * m);
+                v = (v - lo) >> 8;
+              }
+            }
+            const int d = part * (D / 4) + 8 * k + 4 * b;
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
-              const int lo = (int)(int8_t)v;
-              digit[q] |= (uint32_t)(lo & 255) << (8 * k);
-              v = (v - lo) >> 8;
+              const int col = 24 * c + 8 * q + j;
+              const uint32_t chunk16 = D == 64 ? (d >> 4) ^ ((col >> 1) & 3) : (d >> 4) ^ (col & 7);
+              asm volatile("st.shared.u32 [%0], %1;" ::"r"(sb + C::O_Q + buf * C::Q_BYTES + col * D + chunk16 * 16 + (d & 15)), "r"(digit[q]) : "memory");
             }
-          }
-#pragma unroll
-          for (int q = 0; q < 3; ++q) {
-            const int col = 24 * c + 8 * q + j, d = lane * (D / 32);
-            const uint32_t chunk16 = D == 64 ? (d >> 4) ^ ((col >> 1) & 3) : (d >> 4) ^ (col & 7);
-            const uint32_t to = sb + C::O_Q + buf * C::Q_BYTES + col * D + chunk16 * 16 + (d & 15);
-            if (D == 64) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((uint16_t)digit[q]) : "memory");
-            else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(digit[q]) : "memory");
           }
         }
       }
@@ -529,7 +543,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         }
         threads_meet<SOFT>();
       }
-      if (!whole) attn_combine<D, R, SOFT, C::PART_FLOATS>(a, at, s.qt, s.h, s.chunk, begin + (end - begin - at.left) - s.first, per, misc + 7);
+      if (!whole) attn_combine<D, R, SOFT, C::PART_FLOATS>(a, at, s.qt, s.h, s.chunk, begin + (end - begin - at.left) - s.first, per, misc + 7, join);
       if (threadIdx.x == 0) {
         for (int g = 0; g < GROUPS; ++g) broken[g] = 0;
         mbar_arrive(bar_qempty + 8 * buf);                                            // queries, factors and statistics of the unit are done with
@@ -556,7 +570,7 @@ int launch_as(AttnArgs& a, cudaStream_t st) {
   RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page));
   static std::atomic<uint64_t> allowed{0};
   RAZER_TRY(allow_smem((const void*)attn_kv8_few_kernel<D, R>, C::SMEM_BYTES, allowed));
-  return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R>, sm_count(), C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
+  return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R>, sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS, C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
 }
 
 }  // namespace
