@@ -68,6 +68,37 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16])
       "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
+// Pairs of FP32 numbers, two a instruction.
+__device__ __forceinline__ uint64_t pair64(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float low64(uint64_t v) {
+  float lo, hi;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+  return lo;
+}
+__device__ __forceinline__ float high64(uint64_t v) {
+  float lo, hi;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+  return hi;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 // f16 MMAs, A from shared memory or TMEM
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -181,6 +212,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
           }
           lg = vs >= 0.0f && vs < INFINITY ? log2f(vs) : __uint_as_float(0x7FC00000u);   // -infinity for 0
+          if (ks < 0.0f) ks = __uint_as_float(0x7FC00000u);
         }
         const int live = min(boxes, ((g.keys - t * TK - 1) >> a.c.page_log2) + 1);
         const int page = __shfl_sync(0xFFFFFFFFu, id, (block0 - have + lane) & 31);
@@ -360,27 +392,31 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           if (!mbar_wait(bar_s + 8 * t, (uint32_t)(item & 1), abort_flag)) fail(10);
           __syncwarp();
           tc_fence_after();
-          float c[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) c[x] = sc[x].x * f1;
-          // ---- the tile's maximum
+          // ---- the tile's maximum: of sixteen scores before their page's scale, which is not negative
           float most = -INFINITY;
+          bool usual = true;                                                           // factors of the scores that one FP32 number holds
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             uint32_t v[32];
             tc_ld32(t_s + 32 * q, v);
             if (edge) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) most = fmaxf(most, tok0 + 32 * q + x < see ? __uint_as_float(v[x]) * c[2 * q + x / 16] : -INFINITY);
-            } else {
+              for (int x = 0; x < 32; ++x) v[x] = tok0 + 32 * q + x < see ? v[x] : 0xFF800000u;
+            }
 #pragma unroll
-              for (int x = 0; x < 32; ++x) most = fmaxf(most, __uint_as_float(v[x]) * c[2 * q + x / 16]);
+            for (int h = 0; h < 2; ++h) {
+              float top = __uint_as_float(v[16 * h]);
+#pragma unroll
+              for (int x = 1; x < 16; ++x) top = fmaxf(top, __uint_as_float(v[16 * h + x]));
+              const float c = sc[2 * q + h].x * f1, cf = c * f2;
+              usual = usual && (cf == 0.0f ? c == 0.0f : fabsf(cf) > 1e-30f);
+              if (top > -INFINITY) most = fmaxf(most, top * c);
             }
           }
           most = most == -INFINITY ? most : most * f2;
           float fm = 1.0f;
           bool move = false;
-          if (most > m + LAG || (m == -INFINITY && most > m)) {
+          if (most > m + LAG) {                                                        // (or the first)
             fm = ex2(m - most);
             l *= fm;
             m = most;
@@ -401,25 +437,52 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
               tc_st32(t_o + 32 * q, v);
             }
           }
-          // ---- probabilities, over the scores
+          // ---- probabilities, over the scores: exp2(s cf - m), times the value scale of the page over the largest
           const float m0 = m == -INFINITY ? 0.0f : m, lg0 = lg_ref == -INFINITY ? 0.0f : lg_ref;
+          if (!edge && __all_sync(0xFFFFFFFFu, usual)) {
+            uint64_t sum = 0;                                                          // of even and odd columns
+            const uint64_t minus_m = pair64(-m0, -m0);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t v[32], p[16];
-            tc_ld32(t_s + 32 * q, v);
-            const float rel[2] = {ex2(sc[2 * q].y - lg0) * P_ONE, ex2(sc[2 * q + 1].y - lg0) * P_ONE};
+            for (int q = 0; q < 4; ++q) {
+              uint32_t v[32], p[16];
+              tc_ld32(t_s + 32 * q, v);
 #pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              float e0 = ex2(__fmaf_rn(__uint_as_float(v[x]) * c[2 * q + x / 16], f2, -m0)), e1 = ex2(__fmaf_rn(__uint_as_float(v[x + 1]) * c[2 * q + x / 16], f2, -m0));
-              float w0 = e0 * rel[x / 16], w1 = e1 * rel[x / 16];
-              if (edge) {
-                if (tok0 + 32 * q + x >= see) e0 = w0 = 0.0f;
-                if (tok0 + 32 * q + x + 1 >= see) e1 = w1 = 0.0f;
+              for (int h = 0; h < 2; ++h) {
+                const float cf = sc[2 * q + h].x * f1 * f2, rel = ex2(sc[2 * q + h].y - lg0) * P_ONE;
+                const uint64_t cf2 = pair64(cf, cf), rel2 = pair64(rel, rel);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                  const uint64_t z = fma2(pair64(__uint_as_float(v[16 * h + 2 * x]), __uint_as_float(v[16 * h + 2 * x + 1])), cf2, minus_m);
+                  const uint64_t e = pair64(ex2(low64(z)), ex2(high64(z)));
+                  sum = add2(sum, e);
+                  const uint64_t w = mul2(e, rel2);
+                  p[8 * h + x] = pack_half(low64(w), high64(w));
+                }
               }
-              l += e0 + e1;
-              p[x / 2] = pack_half(w0, w1);
+              tc_st16(t_s + 16 * q, p);
             }
-            tc_st16(t_s + 16 * q, p);
+            l += low64(sum) + high64(sum);
+          } else {
+#pragma unroll 1
+            for (int q = 0; q < 8; ++q) {                                              // sixteen columns at a time
+              uint32_t v[16], p[8];
+              tc_ld16(t_s + 16 * q, v);
+              tc_wait_ld();
+              const float c = sc[q].x * f1, rel = ex2(sc[q].y - lg0) * P_ONE;
+#pragma unroll
+              for (int x = 0; x < 16; x += 2) {
+                float e[2], w[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const bool seen = tok0 + 16 * q + x + k < see;                       // a scale that is NaN is not the hidden rows' affair
+                  e[k] = seen ? ex2(__fmaf_rn(__uint_as_float(v[x + k]) * c, f2, -m0)) : 0.0f;
+                  w[k] = seen ? e[k] * rel : 0.0f;
+                }
+                l += e[0] + e[1];
+                p[x / 2] = pack_half(w[0], w[1]);
+              }
+              tc_st8(t_s + 8 * q, p);
+            }
           }
           tc_wait_st();
           tc_fence_before();
