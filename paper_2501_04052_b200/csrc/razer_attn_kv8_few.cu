@@ -114,12 +114,12 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     }
     for (int i = 0; i < GROUPS; ++i) {
       mbar_init(bar_sfull + 8 * i, 1);
-      mbar_init(bar_pfull + 8 * i, 128);
+      mbar_init(bar_pfull + 8 * i, 4);                   // a warp arrives by one lane: 32 arrivals of a warp take their turns
       mbar_init(bar_ofull + 8 * i, 1);
       broken[i] = 0;
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar_qfull + 8 * i, 32);
+      mbar_init(bar_qfull + 8 * i, 1);
       mbar_init(bar_qempty + 8 * i, 1);
     }
     mbar_init(bar_drain, 1);
@@ -290,7 +290,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(bar_qfull + 8 * buf);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_qfull + 8 * buf);
       if (!walk_advance(a, TK, at, g.n_items)) break;
     }
   } else if (warp == C::W_MMA) {
@@ -482,7 +483,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
-        mbar_arrive(bar_pfull + 8 * group);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_pfull + 8 * group);
         if (CHUNKS == 1 && pending) take(0, reinterpret_cast<uint32_t(&)[24]>(x_o), table + ((mine - 1) % C::TABLES) * R * 8);
         pending = true;
       }

@@ -4,8 +4,9 @@
 // 1152 + code, and a packed subtraction leaves the code; 5 instructions for 4 codes, paid once for 256 rows) in the layout of the MMA's B
 // operand, one warp issues
 //   S = Q K^T  (128 x 128, FP32 in TMEM)   and   O += P V  (P from TMEM, over S)
-// for the two tiles in turn, so that one tile's products run under the other one's softmax.  A thread has a row: maximum and sum take no
-// shuffle.  O stays in TMEM; it is brought to a new maximum only when that has grown by more than 2^8, so that after a unit's first tiles next to
+// for the two tiles in turn, so that one tile's products run under the other one's softmax.  Two threads have a row, 64 columns
+// each, and tell each other the maximum through shared memory (with one thread a row the softmax was a chain of 4100 cycles a tile that nothing
+// hid).  O stays in TMEM; it is brought to a new maximum only when that has grown by more than 2^8, so that after a unit's first tiles next to
 // never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16 times 2^6
 // (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to the largest met.
 // What bounds it: the exponentials (16 a cycle: 2048 cycles a tile of 256 x 128) and the MMAs (2048) alike, then the softmax's issue.
@@ -25,7 +26,7 @@ constexpr float LAG = 8.0f;                              // how far (log2) a max
 template <int D_>
 struct ManyCfg {
   static constexpr int D = D_, R = 256, TK = 128;
-  static constexpr int THREADS = 448, W_LOAD = 12, W_MMA = 13;         // warps 0-3, 4-7: softmax of a row tile each; 8-11: codes to f16
+  static constexpr int SOFT = 512, THREADS = 704, W_CODES = 16, W_LOAD = 20, W_MMA = 21;   // warps 0-7, 8-15: softmax of a row tile each; 16-19: codes to f16
   static constexpr int HALF_BYTES = TK * D * 2, TILE_BYTES = TK * D;
   static constexpr int O_Q = 0;                                        // [tile][block][128 rows][128 bytes]
   static constexpr int O_K = 2 * HALF_BYTES;                           // two buffers [block][128 tokens][128 bytes]
@@ -34,8 +35,9 @@ struct ManyCfg {
   static constexpr int O_META = O_CODES + 2 * TILE_BYTES;              // [4][8] {key scale, log2 of the value scale}, [4] the largest of the latter
   static constexpr int O_BAR = O_META + 4 * 72;
   static constexpr int N_BAR = 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 1;
-  static constexpr int O_MISC = O_BAR + 8 * N_BAR;
-  static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
+  static constexpr int O_MISC = O_BAR + 8 * N_BAR;                     // (256 bytes)
+  static constexpr int O_TOP = O_MISC + 256;                           // [tile][half][128 rows]: maxima, at the end sums
+  static constexpr int SMEM_BYTES = O_TOP + 2048;
   static constexpr int PART_FLOATS = R * (D + 3);                      // [D][R] O, [R] ta, tm, sum
 };
 
@@ -62,12 +64,6 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&v)[32]) {
       : "memory");
   tc_wait_ld();
 }
-__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
-      "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
 // Pairs of FP32 numbers, two a instruction.
 __device__ __forceinline__ uint64_t pair64(float lo, float hi) {
   uint64_t r;
@@ -75,13 +71,13 @@ __device__ __forceinline__ uint64_t pair64(float lo, float hi) {
   return r;
 }
 __device__ __forceinline__ float low64(uint64_t v) {
-  float lo, hi;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+  float lo;
+  asm("{\n\t.reg .f32 hi;\n\tmov.b64 {%0, hi}, %1;\n\t}" : "=f"(lo) : "l"(v));
   return lo;
 }
 __device__ __forceinline__ float high64(uint64_t v) {
-  float lo, hi;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+  float hi;
+  asm("{\n\t.reg .f32 lo;\n\tmov.b64 {lo, %0}, %1;\n\t}" : "=f"(hi) : "l"(v));
   return hi;
 }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
@@ -121,13 +117,18 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, ui
 }
 
 template <int D>
-__global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+__global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                const __grid_constant__ AttnArgs a) {
   using C = ManyCfg<D>;
   constexpr int TK = C::TK, R = C::R;
-  extern __shared__ uint8_t attn_smem[];
-  uint8_t* sm = attn_smem + ((1024 - (smem_u32(attn_smem) & 1023)) & 1023);
+  // Swizzled tiles want 1024-byte boundaries.  Dynamic shared memory begins on one where a kernel has no other; a launch where it does not would say so.
+  extern __shared__ __align__(1024) uint8_t attn_many_smem[];
+  uint8_t* sm = attn_many_smem;
   const uint32_t sb = smem_u32(sm);
+  if (sb & 1023) {
+    if (threadIdx.x == 0) atomicCAS(a.status, 0u, 12u);
+    return;
+  }
   // codes of keys / values in and read; f16 buffers ready and free; queries ready; S, P; O of a unit
   const uint32_t bar = sb + C::O_BAR;
   const uint32_t bar_in = bar, bar_read = bar + 16, bar_kready = bar + 32, bar_kfree = bar + 48, bar_vready = bar + 64, bar_vfree = bar + 80, bar_q = bar + 96,
@@ -142,14 +143,14 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_in + 8 * i, 1);
-      mbar_init(bar_read + 8 * i, 128);
-      mbar_init(bar_kready + 8 * i, 128);
+      mbar_init(bar_read + 8 * i, 4);                    // a warp arrives by one lane: 32 arrivals of a warp take their turns
+      mbar_init(bar_kready + 8 * i, 4);
       mbar_init(bar_kfree + 8 * i, 1);
-      mbar_init(bar_vready + 8 * i, 128);
+      mbar_init(bar_vready + 8 * i, 4);
       mbar_init(bar_vfree + 8 * i, 1);
-      mbar_init(bar_q + 8 * i, 128);
+      mbar_init(bar_q + 8 * i, 8);
       mbar_init(bar_s + 8 * i, 1);
-      mbar_init(bar_p + 8 * i, 128);
+      mbar_init(bar_p + 8 * i, 8);
       mbar_init(bar_o + 8 * i, 1);
     }
     mbar_init(bar_drain, 1);
@@ -253,9 +254,9 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
     // copies in flight must land before shared memory is released
     if (item > 0) mbar_wait(bar_in, (uint32_t)((item - 1) & 1), never);
     if (asked_v > 0) mbar_wait(bar_in + 8, (uint32_t)((asked_v - 1) & 1), never);
-  } else if (warp >= 8 && warp < 12) {
+  } else if (warp >= C::W_CODES && warp < C::W_LOAD) {
     // ===================== codes to f16: a thread a token =====================
-    const int tok = threadIdx.x - 256;
+    const int tok = threadIdx.x - C::SOFT;
     const uint32_t row_in = sb + C::O_CODES + tok * D;
     int item = 0;
     do {
@@ -277,9 +278,12 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             sts128(at16 + ((c0 ^ (tok & 7)) << 4), half_pair(w.x), half_pair(w.x >> 8), half_pair(w.y), half_pair(w.y >> 8));
             sts128(at16 + (((c0 + 1) ^ (tok & 7)) << 4), half_pair(w.z), half_pair(w.z >> 8), half_pair(w.w), half_pair(w.w >> 8));
           }
-          mbar_arrive(bar_read + 8 * which);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          mbar_arrive(ready);
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(ready);
+            mbar_arrive(bar_read + 8 * which);
+          }
         }
       }
       if (!walk_advance(a, TK, at, g.n_items)) break;
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         tc_fence_after();
         const uint32_t v = sb + C::O_V + (i & 1) * C::HALF_BYTES;
 #pragma unroll
-        for (int k = 0; k < TK / 16; ++k) mma_ts(tmem_o + 128 * t, tmem + 128 * t + 8 * k, lo(v + k * 2048, TK * 128 / 16), hi, id_o, !fresh || k > 0);
+        for (int k = 0; k < TK / 16; ++k) mma_ts(tmem_o + 128 * t, tmem + 128 * t + 64 * (k / 4) + 8 * (k % 4), lo(v + k * 2048, TK * 128 / 16), hi, id_o, !fresh || k > 0);
       };
       for (;;) {
         const Seg g = segment(at);
@@ -341,10 +345,13 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
     __syncwarp();
     mbar_wait(bar_drain, 0, never);
     __syncwarp();
-  } else if (warp < 8) {
-    // ===================== softmax: a thread a row =====================
-    const int t = warp >> 2, row = 128 * t + 32 * (warp & 3) + lane;                  // of the unit
-    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + lanes + 128 * t, t_o = tmem_o + lanes + 128 * t;
+  } else if (warp < C::W_CODES) {
+    // ===================== softmax: two threads a row =====================
+    const int t = warp >> 3, half = (warp >> 2) & 1, row = 128 * t + 32 * (warp & 3) + lane;   // of the unit
+    float* top_mine = reinterpret_cast<float*>(sm + C::O_TOP) + (2 * t + half) * 128 + (row & 127);
+    const float* top_other = reinterpret_cast<float*>(sm + C::O_TOP) + (2 * t + (half ^ 1)) * 128 + (row & 127);
+    auto row_meet = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + lanes + 128 * t, t_o = tmem_o + lanes + 128 * t + half * (D / 2);
     int item = 0, units = 0;
     for (;;) {
       const Seg g = segment(at);
@@ -353,15 +360,19 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       const int see = real ? max(at.len - at.n + i + 1, 0) : 0x7FFFFFFF;
       float m = -INFINITY, l = 0.0f, lg_ref = -INFINITY, f1 = 0.0f, f2 = 0.0f;
       if (g.last > g.first) {
-        // ---- the row of queries
+        // ---- the row of queries, half of it a thread
         uint32_t top = 0;
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D);
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + half * (D / 16);
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
+        for (int c = 0; c < D / 16; ++c) {
           const uint4 x = real ? src[c] : make_uint4(0, 0, 0, 0);
           top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
         }
         top = max(top >> 16, top & 0xFFFFu) << 16;
+        *top_mine = __uint_as_float(top);
+        row_meet();
+        top = max(top, __float_as_uint(*top_other));
+        row_meet();                                                                    // both have read
         const bool bad = top >= 0x7F800000u || kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
         const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
         // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
@@ -370,8 +381,9 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         f2 = power2(e - e / 2 - 14);
         const uint32_t to = sb + C::O_Q + t * C::HALF_BYTES + (row & 127) * 128;
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 x = real && !bad ? src[c] : make_uint4(0, 0, 0, 0);              // (again, from L1)
+        for (int c0 = 0; c0 < D / 16; ++c0) {
+          const int c = half * (D / 16) + c0;
+          const uint4 x = real && !bad ? src[c0] : make_uint4(0, 0, 0, 0);             // (again, from L1)
           uint32_t w[4];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                                               // four dimensions, in the order 0, 2, 1, 3
@@ -382,13 +394,21 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           sts128(to + (c >> 3) * (TK * 128) + (((c & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(bar_q + 8 * t);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_q + 8 * t);
         for (int j = g.first; j < g.last; ++j, ++item) {
           const int tok0 = j * TK;
           const bool edge = __any_sync(0xFFFFFFFFu, tok0 + TK > see);
           if (!mbar_wait(bar_kready + 8 * (item & 1), (uint32_t)((item >> 1) & 1), abort_flag)) fail(9);   // the scales are in place
-          const float2* sc = meta + (item & 3) * 8;
           const float lg_top = meta_top[item & 3];
+          float c[4], lg[4];                                                           // of the half's four times sixteen columns
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float2 sc = meta[(item & 3) * 8 + 4 * half + q];
+            c[q] = sc.x * f1;
+            lg[q] = sc.y;
+          }
+          const int first = tok0 + 64 * half;
           if (!mbar_wait(bar_s + 8 * t, (uint32_t)(item & 1), abort_flag)) fail(10);
           __syncwarp();
           tc_fence_after();
@@ -396,24 +416,27 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           float most = -INFINITY;
           bool usual = true;                                                           // factors of the scores that one FP32 number holds
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < 4; q += 2) {
             uint32_t v[32];
-            tc_ld32(t_s + 32 * q, v);
+            tc_ld32(t_s + 64 * half + 16 * q, v);
             if (edge) {
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = tok0 + 32 * q + x < see ? v[x] : 0xFF800000u;
+              for (int x = 0; x < 32; ++x) v[x] = first + 16 * q + x < see ? v[x] : 0xFF800000u;
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float top = __uint_as_float(v[16 * h]);
+              float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-              for (int x = 1; x < 16; ++x) top = fmaxf(top, __uint_as_float(v[16 * h + x]));
-              const float c = sc[2 * q + h].x * f1, cf = c * f2;
-              usual = usual && (cf == 0.0f ? c == 0.0f : fabsf(cf) > 1e-30f);
-              if (top > -INFINITY) most = fmaxf(most, top * c);
+              for (int x = 0; x < 16; ++x) top[x & 1] = fmaxf(top[x & 1], __uint_as_float(v[16 * h + x]));
+              const float cf = c[q + h] * f2, topmost = fmaxf(top[0], top[1]);
+              usual = usual && (cf == 0.0f ? c[q + h] == 0.0f : fabsf(cf) > 1e-30f);
+              if (topmost > -INFINITY) most = fmaxf(most, topmost * c[q + h]);
             }
           }
           most = most == -INFINITY ? most : most * f2;
+          *top_mine = most;
+          row_meet();                                  // (the next write comes behind the next S, which comes behind both halves' arrivals below)
+          most = fmaxf(most, *top_other);
           float fm = 1.0f;
           bool move = false;
           if (most > m + LAG) {                                                        // (or the first)
@@ -429,7 +452,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           }
           if (j > g.first && __any_sync(0xFFFFFFFFu, move)) {                         // (the last product with the values is over: S came behind it)
 #pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
+            for (int q = 0; q < D / 64; ++q) {
               uint32_t v[32];
               tc_ld32(t_o + 32 * q, v);
 #pragma unroll
@@ -437,61 +460,63 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
               tc_st32(t_o + 32 * q, v);
             }
           }
-          // ---- probabilities, over the scores: exp2(s cf - m), times the value scale of the page over the largest
+          // ---- probabilities, each half's over its own scores: exp2(s cf - m), times the value scale of the page over the largest
           const float m0 = m == -INFINITY ? 0.0f : m, lg0 = lg_ref == -INFINITY ? 0.0f : lg_ref;
           if (!edge && __all_sync(0xFFFFFFFFu, usual)) {
             uint64_t sum = 0;                                                          // of even and odd columns
             const uint64_t minus_m = pair64(-m0, -m0);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              uint32_t v[32], p[16];
-              tc_ld32(t_s + 32 * q, v);
+              uint32_t v[16], p[8];
+              tc_ld16(t_s + 64 * half + 16 * q, v);
+              tc_wait_ld();
+              const float cf = c[q] * f2, rel = ex2(lg[q] - lg0) * P_ONE;
+              const uint64_t cf2 = pair64(cf, cf), rel2 = pair64(rel, rel);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const float cf = sc[2 * q + h].x * f1 * f2, rel = ex2(sc[2 * q + h].y - lg0) * P_ONE;
-                const uint64_t cf2 = pair64(cf, cf), rel2 = pair64(rel, rel);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                  const uint64_t z = fma2(pair64(__uint_as_float(v[16 * h + 2 * x]), __uint_as_float(v[16 * h + 2 * x + 1])), cf2, minus_m);
-                  const uint64_t e = pair64(ex2(low64(z)), ex2(high64(z)));
-                  sum = add2(sum, e);
-                  const uint64_t w = mul2(e, rel2);
-                  p[8 * h + x] = pack_half(low64(w), high64(w));
-                }
+              for (int x = 0; x < 8; ++x) {
+                const uint64_t z = fma2(pair64(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), cf2, minus_m);
+                const uint64_t e = pair64(ex2(low64(z)), ex2(high64(z)));
+                sum = add2(sum, e);
+                const uint64_t w = mul2(e, rel2);
+                p[x] = pack_half(low64(w), high64(w));
               }
-              tc_st16(t_s + 16 * q, p);
+              tc_st8(t_s + 64 * half + 8 * q, p);
             }
             l += low64(sum) + high64(sum);
           } else {
-#pragma unroll 1
-            for (int q = 0; q < 8; ++q) {                                              // sixteen columns at a time
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
               uint32_t v[16], p[8];
-              tc_ld16(t_s + 16 * q, v);
+              tc_ld16(t_s + 64 * half + 16 * q, v);
               tc_wait_ld();
-              const float c = sc[q].x * f1, rel = ex2(sc[q].y - lg0) * P_ONE;
+              const float rel = ex2(lg[q] - lg0) * P_ONE;
 #pragma unroll
               for (int x = 0; x < 16; x += 2) {
                 float e[2], w[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                  const bool seen = tok0 + 16 * q + x + k < see;                       // a scale that is NaN is not the hidden rows' affair
-                  e[k] = seen ? ex2(__fmaf_rn(__uint_as_float(v[x + k]) * c, f2, -m0)) : 0.0f;
+                  const bool seen = first + 16 * q + x + k < see;                      // a scale that is NaN is not the hidden rows' affair
+                  e[k] = seen ? ex2(__fmaf_rn(__uint_as_float(v[x + k]) * c[q], f2, -m0)) : 0.0f;
                   w[k] = seen ? e[k] * rel : 0.0f;
                 }
                 l += e[0] + e[1];
                 p[x / 2] = pack_half(w[0], w[1]);
               }
-              tc_st8(t_s + 8 * q, p);
+              tc_st8(t_s + 64 * half + 8 * q, p);
             }
           }
           tc_wait_st();
           tc_fence_before();
-          mbar_arrive(bar_p + 8 * t);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_p + 8 * t);
         }
         if (!mbar_wait(bar_o + 8 * t, (uint32_t)(units & 1), abort_flag)) fail(11);
         __syncwarp();
         tc_fence_after();
         ++units;
+        *top_mine = l;
+        row_meet();
+        l += *top_other;
       }
       // ---- the end of the unit.  lg_ref may be -infinity: nothing but values of scale 0 was met, and O is 0
       const bool whole = g.first == 0 && g.n_items == at.tiles, any = g.last > g.first;
@@ -499,7 +524,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       const long long out_row = (long long)(at.row0 + i) * a.c.heads * a.G + g.h * a.G + hq;
       float* part = a.parts + ((long long)blockIdx.x * 2 + (g.first > 0 ? 0 : 1)) * C::PART_FLOATS;
 #pragma unroll 1
-      for (int q = 0; q < D / 32; ++q) {
+      for (int q = 0; q < D / 64; ++q) {
+        const int d0 = half * (D / 2) + 32 * q;
         uint32_t v[32];
         if (any) tc_ld32(t_o + 32 * q, v);
 #pragma unroll
@@ -508,29 +534,31 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           if (real) {
 #pragma unroll
             for (int x = 0; x < 32; x += 4)                                            // columns 0, 2, 1, 3 of four
-              attn_store<D>(a, out_row, 32 * q + x, make_float4(__uint_as_float(v[x]), __uint_as_float(v[x + 2]), __uint_as_float(v[x + 1]), __uint_as_float(v[x + 3])), l, ta, m);
+              attn_store<D>(a, out_row, d0 + x, make_float4(__uint_as_float(v[x]), __uint_as_float(v[x + 2]), __uint_as_float(v[x + 1]), __uint_as_float(v[x + 3])), l, ta, m);
           }
         } else {
 #pragma unroll
-          for (int x = 0; x < 32; ++x) __stcg(part + (32 * q + x) * R + row, __uint_as_float(v[x]));
+          for (int x = 0; x < 32; ++x) __stcg(part + (d0 + x) * R + row, __uint_as_float(v[x]));
         }
       }
       tc_fence_before();
       if (!whole) {
-        __stcg(part + D * R + row, ta);
-        __stcg(part + D * R + R + row, m);
-        __stcg(part + D * R + 2 * R + row, l);
-        // the last of the unit's CTAs to get here adds the parts up, a thread a row
+        if (half == 0) {
+          __stcg(part + D * R + row, ta);
+          __stcg(part + D * R + R + row, m);
+          __stcg(part + D * R + 2 * R + row, l);
+        }
+        // the last of the unit's CTAs to get here adds the parts up, half a row a thread
         const long long unit_begin = begin + (end - begin - at.left) - g.first;
         const int c_first = (int)(unit_begin / per), parts = (int)((unit_begin + at.tiles - 1) / per) - c_first + 1;
-        threads_meet<256>();
+        threads_meet<C::SOFT>();
         if (threadIdx.x == 0) {
           uint32_t seen;
           asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.counters + c_first) : "memory");
           misc[7] = seen == (uint32_t)(parts - 1);
           if (misc[7]) a.counters[c_first] = 0;
         }
-        threads_meet<256>();
+        threads_meet<C::SOFT>();
         if (misc[7]) {
           auto at_part = [&](int c) { return a.parts + ((long long)(c_first + c) * 2 + (c == 0)) * C::PART_FLOATS + row; };
           float top_a = -INFINITY, top_m = -INFINITY, sum_l = 0.0f;
@@ -541,7 +569,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             top_m = nm;
           }
 #pragma unroll 1
-          for (int d = 0; d < D; d += 8) {
+          for (int d = half * (D / 2); d < (half + 1) * (D / 2); d += 8) {
             float sum[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) sum[x] = 0.0f;
@@ -558,7 +586,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             }
           }
         }
-        threads_meet<256>();                                                           // misc[7] has been read
+        threads_meet<C::SOFT>();                                                           // misc[7] has been read
       }
       if (!walk_advance(a, TK, at, g.n_items)) break;
     }
