@@ -3,13 +3,15 @@
 // Two row tiles of 128 share every tile of 128 tokens.  Four warps turn its codes into f16 (exact: byte ^ 0x80 under an exponent of 2^10 is
 // 1152 + code, and a packed subtraction leaves the code; 5 instructions for 4 codes, paid once for 256 rows) in the layout of the MMA's B
 // operand, one warp issues
-//   S = Q K^T  (128 x 128, FP32 in TMEM)   and   O += P V  (P from TMEM, over S)
-// for the two tiles in turn, so that one tile's products run under the other one's softmax.  Two threads have a row, 64 columns
-// each, and tell each other the maximum through shared memory (with one thread a row the softmax was a chain of 4100 cycles a tile that nothing
-// hid).  O stays in TMEM; it is brought to a new maximum only when that has grown by more than 2^8, so that after a unit's first tiles next to
-// never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16 times 2^6
-// (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to the largest met.
-// What bounds it: the exponentials (16 a cycle: 2048 cycles a tile of 256 x 128) and the MMAs (2048) alike, then the softmax's issue.
+//   S = Q K^T  (128 x 64, FP32 in TMEM)   and   O += P V  (P from TMEM, over S)
+// in steps of 64 tokens.  S has two buffers a row tile, so that the next scores are there when a softmax is done with the last (with one buffer of 128
+// columns a row tile's softmax and products took turns: 6000 cycles a tile).  A thread has a row: maximum and sum take no shuffle, the step's
+// scores are read once.  O stays in TMEM; it is brought to a new maximum only when that has grown by more than 2^8, so that after a unit's
+// first tiles next to never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16
+// times 2^6 (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to
+// twice the largest met.
+// What bounds it: the exponentials (16 a cycle: 2048 cycles a tile of 256 x 128), the MMAs (2800, those of S half as wide as they are long), and the chain of one
+// step's softmax.
 // Row tiles of a sequence are taken in the order first, last, second, last but one ..., so that equal runs of them are about equal work under the
 // causal mask.  Work is cut among the CTAs as razer_attn_kv8.cuh says.
 #include "razer_attn_kv8.cuh"
@@ -26,19 +28,27 @@ constexpr float LAG = 8.0f;                              // how far (log2) a max
 template <int D_>
 struct ManyCfg {
   static constexpr int D = D_, R = 256, TK = 128;
-  static constexpr int SOFT = 512, THREADS = 704, W_CODES = 16, W_LOAD = 20, W_MMA = 21;   // warps 0-7, 8-15: softmax of a row tile each; 16-19: codes to f16
+  static constexpr int SOFT = 256, THREADS = 448, W_CODES = 8, W_LOAD = 12, W_MMA = 13;   // warps 0-3, 4-7: softmax of a row tile each; 8-11: codes to f16
+  static constexpr int STEP = 64;                                      // tokens of a step
   static constexpr int HALF_BYTES = TK * D * 2, TILE_BYTES = TK * D;
   static constexpr int O_Q = 0;                                        // [tile][block][128 rows][128 bytes]
-  static constexpr int O_K = 2 * HALF_BYTES;                           // two buffers [block][128 tokens][128 bytes]
-  static constexpr int O_V = O_K + 2 * HALF_BYTES;
-  static constexpr int O_CODES = O_V + 2 * HALF_BYTES;                 // keys, values: [128 tokens][D]
-  static constexpr int O_META = O_CODES + 2 * TILE_BYTES;              // [4][8] {key scale, log2 of the value scale}, [4] the largest of the latter
-  static constexpr int O_BAR = O_META + 4 * 72;
-  static constexpr int N_BAR = 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 2 + 1;
-  static constexpr int O_MISC = O_BAR + 8 * N_BAR;                     // (256 bytes)
-  static constexpr int O_TOP = O_MISC + 256;                           // [tile][half][128 rows]: maxima, at the end sums
-  static constexpr int SMEM_BYTES = O_TOP + 2048;
+  static constexpr int O_K = 2 * HALF_BYTES;                           // [block][128 tokens][128 bytes]
+  static constexpr int O_V = O_K + HALF_BYTES;                         // two buffers: the next tile's are made while products still read the last one's
+  static constexpr int STAGES = 2;                                     // of codes: with one, a copy's latency was in every tile (194 us of 458 were that skeleton)
+  static constexpr int O_CODES = O_V + 2 * HALF_BYTES;                     // keys, values of each stage: [128 tokens][D]
+  static constexpr int METAS = 8;                                      // tiles whose scales are held: two on their way, up to three in work
+  static constexpr int O_META = O_CODES + 2 * STAGES * TILE_BYTES;     // [METAS][8] {key scale, log2 of the value scale}, [METAS] the largest of the latter
+  static constexpr int O_BAR = O_META + METAS * 68;
+  static constexpr int N_BAR = 4 * STAGES + 6 + 2 + 4 + 4 + 4 + 1;
+  static constexpr int O_MISC = O_BAR + 8 * N_BAR;
+  static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
   static constexpr int PART_FLOATS = R * (D + 3);                      // [D][R] O, [R] ta, tm, sum
+};
+
+// A Walk and its run's bounds.
+struct Held {
+  int b, row0, n, len, tiles, units, unit, tile;
+  long long left, begin, end, per;
 };
 
 __device__ __forceinline__ uint32_t half_pair(uint32_t bytes02) {        // codes in bytes 0 and 2 -> f16 pair
@@ -62,7 +72,6 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&v)[32]) {
         "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
       : "r"(taddr)
       : "memory");
-  tc_wait_ld();
 }
 // Pairs of FP32 numbers, two a instruction.
 __device__ __forceinline__ uint64_t pair64(float lo, float hi) {
@@ -117,41 +126,43 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, ui
 }
 
 template <int D>
-__global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+__global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                const __grid_constant__ AttnArgs a) {
   using C = ManyCfg<D>;
   constexpr int TK = C::TK, R = C::R;
-  // Swizzled tiles want 1024-byte boundaries.  Dynamic shared memory begins on one where a kernel has no other; a launch where it does not would say so.
-  extern __shared__ __align__(1024) uint8_t attn_many_smem[];
-  uint8_t* sm = attn_many_smem;
+  extern __shared__ uint8_t attn_smem[];
+  uint8_t* sm = attn_smem + ((1024 - (smem_u32(attn_smem) & 1023)) & 1023);
   const uint32_t sb = smem_u32(sm);
-  if (sb & 1023) {
-    if (threadIdx.x == 0) atomicCAS(a.status, 0u, 12u);
-    return;
-  }
-  // codes of keys / values in and read; f16 buffers ready and free; queries ready; S, P; O of a unit
+  // codes of keys / values in and read; f16 buffers ready and free; queries ready; S, P; products with the values done
   const uint32_t bar = sb + C::O_BAR;
-  const uint32_t bar_in = bar, bar_read = bar + 16, bar_kready = bar + 32, bar_kfree = bar + 48, bar_vready = bar + 64, bar_vfree = bar + 80, bar_q = bar + 96,
-                 bar_s = bar + 112, bar_p = bar + 128, bar_o = bar + 144, bar_drain = bar + 160;
+  const uint32_t bar_in = bar, bar_read = bar_in + 16 * C::STAGES, bar_kready = bar_read + 16 * C::STAGES, bar_kfree = bar_kready + 8, bar_vready = bar_kfree + 8,
+                 bar_vfree = bar_vready + 16, bar_q = bar_vfree + 16, bar_s = bar_q + 16, bar_p = bar_s + 32, bar_o = bar_p + 32, bar_drain = bar_o + 32;   // in, read: [keys, values][stage]; s, p, o: [row tile][buffer]
   int* misc = reinterpret_cast<int*>(sm + C::O_MISC);                    // abort, never set, share (4 words), TMEM, last; sums from word 16
   volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(misc);
   volatile uint32_t* never = reinterpret_cast<uint32_t*>(misc + 1);
   float2* meta = reinterpret_cast<float2*>(sm + C::O_META);
-  float* meta_top = reinterpret_cast<float*>(meta + 32);
+  float* meta_top = reinterpret_cast<float*>(meta + 8 * C::METAS);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 2 * C::STAGES; ++i) {
       mbar_init(bar_in + 8 * i, 1);
-      mbar_init(bar_read + 8 * i, 4);                    // a warp arrives by one lane: 32 arrivals of a warp take their turns
-      mbar_init(bar_kready + 8 * i, 4);
-      mbar_init(bar_kfree + 8 * i, 1);
+      mbar_init(bar_read + 8 * i, 4);              // a warp arrives by one lane: 32 arrivals of a warp take their turns
+    }
+    mbar_init(bar_kready, 4);
+    mbar_init(bar_kfree, 1);
+    for (int i = 0; i < 2; ++i) {
       mbar_init(bar_vready + 8 * i, 4);
       mbar_init(bar_vfree + 8 * i, 1);
-      mbar_init(bar_q + 8 * i, 8);
-      mbar_init(bar_s + 8 * i, 1);
-      mbar_init(bar_p + 8 * i, 8);
-      mbar_init(bar_o + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_q + 8 * i, 4);
+      mbar_init(bar_s + 16 * i, 1);
+      mbar_init(bar_s + 16 * i + 8, 1);
+      mbar_init(bar_p + 16 * i, 4);
+      mbar_init(bar_p + 16 * i + 8, 4);
+      mbar_init(bar_o + 16 * i, 1);
+      mbar_init(bar_o + 16 * i + 8, 1);
     }
     mbar_init(bar_drain, 1);
     misc[0] = misc[1] = 0;
@@ -170,13 +181,13 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
   Walk at;
   const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at);
   tc_fence_after();
-  const uint32_t tmem = (uint32_t)misc[6], tmem_o = tmem + 256;        // S and P: 128 columns a row tile; O behind
+  const uint32_t tmem = (uint32_t)misc[6], tmem_o = tmem + 256;        // S and P: two buffers of 64 columns a row tile; O behind
   auto fail = [&](uint32_t code) {
     *abort_flag = 1;
     atomicCAS(a.status, 0u, code);
   };
   // A segment.  Units of a sequence: head by head, row tiles from both ends.
-  struct Seg { int n_items, qt, h, chunk, keys, first, last; };
+  struct Seg { int n_items, qt, h, chunk, keys, first, last, steps; };
   auto segment = [&](const Walk& at) {
     Seg g;
     g.n_items = walk_count(at);
@@ -187,6 +198,7 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
     g.keys = max(at.len - at.n + min((g.qt + 1) * a.tq, at.n), 0);
     g.first = at.tile;
     g.last = max(min(at.tile + g.n_items, (g.keys + TK - 1) / TK), g.first);
+    g.steps = g.last > g.first ? min(2 * (g.last - g.first), (g.keys - g.first * TK + C::STEP - 1) / C::STEP) : 0;
     return g;
   };
 
@@ -224,24 +236,26 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
         float most = v1;
         for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
         if (!(most > -INFINITY)) most = -INFINITY;
-        if (item > 0) {                                          // the codes before have been read
-          if (!mbar_wait(bar_read, (uint32_t)((item - 1) & 1), abort_flag)) fail(1), alive = false;
+        const int stage = item % C::STAGES, round = item / C::STAGES;
+        if (round > 0) {                                         // the codes before have been read
+          if (!mbar_wait(bar_read + 8 * stage, (uint32_t)(round & 1) ^ 1u, abort_flag)) fail(1), alive = false;
           alive = __all_sync(0xFFFFFFFFu, alive);
           if (!alive) break;
         }
-        if (lane < 8) meta[(item & 3) * 8 + lane] = make_float2(k1, v1);
-        if (lane == 0) meta_top[item & 3] = most;
+        if (lane < 8) meta[item % C::METAS * 8 + lane] = make_float2(k1, v1);
+        if (lane == 0) meta_top[item % C::METAS] = most;
         __syncwarp();
         auto bring = [&](const CUtensorMap* map, int which) {
-          if (lane == 0) mbar_expect_tx(bar_in + 8 * which, (uint32_t)((live << a.c.page_log2) * D));
+          const uint32_t in = bar_in + 8 * (which * C::STAGES + stage);
+          if (lane == 0) mbar_expect_tx(in, (uint32_t)((live << a.c.page_log2) * D));
           __syncwarp();
           if (lane < live)
-            tma_load_3d(sb + C::O_CODES + which * C::TILE_BYTES + (uint32_t)((lane << a.c.page_log2) * D), map, 0, 0, max(page, 0) * a.c.heads + g.h, bar_in + 8 * which);
+            tma_load_3d(sb + C::O_CODES + (2 * stage + which) * C::TILE_BYTES + (uint32_t)((lane << a.c.page_log2) * D), map, 0, 0, max(page, 0) * a.c.heads + g.h, in);
           __syncwarp();
         };
         bring(&map_k, 0);
-        if (item > 0) {
-          if (!mbar_wait(bar_read + 8, (uint32_t)((item - 1) & 1), abort_flag)) fail(2), alive = false;
+        if (round > 0) {
+          if (!mbar_wait(bar_read + 8 * (C::STAGES + stage), (uint32_t)(round & 1) ^ 1u, abort_flag)) fail(2), alive = false;
           alive = __all_sync(0xFFFFFFFFu, alive);
           if (!alive) { ++item; break; }
         }
@@ -252,27 +266,28 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
       if (!walk_advance(a, TK, at, g.n_items)) break;
     } while (true);
     // copies in flight must land before shared memory is released
-    if (item > 0) mbar_wait(bar_in, (uint32_t)((item - 1) & 1), never);
-    if (asked_v > 0) mbar_wait(bar_in + 8, (uint32_t)((asked_v - 1) & 1), never);
+    for (int f = max(item - C::STAGES, 0); f < item; ++f) mbar_wait(bar_in + 8 * (f % C::STAGES), (uint32_t)((f / C::STAGES) & 1), never);
+    for (int f = max(asked_v - C::STAGES, 0); f < asked_v; ++f) mbar_wait(bar_in + 8 * (C::STAGES + f % C::STAGES), (uint32_t)((f / C::STAGES) & 1), never);
   } else if (warp >= C::W_CODES && warp < C::W_LOAD) {
     // ===================== codes to f16: a thread a token =====================
     const int tok = threadIdx.x - C::SOFT;
-    const uint32_t row_in = sb + C::O_CODES + tok * D;
     int item = 0;
     do {
       const Seg g = segment(at);
       for (int t = g.first; t < g.last; ++t, ++item) {
-        const int buf = item & 1;
+        const int stage = item % C::STAGES;
 #pragma unroll 1
         for (int which = 0; which < 2; ++which) {
-          const uint32_t free_bar = (which ? bar_vfree : bar_kfree) + 8 * buf, ready = (which ? bar_vready : bar_kready) + 8 * buf;
-          if (!mbar_wait(bar_in + 8 * which, (uint32_t)(item & 1), abort_flag)) fail(3);
-          if (item >= 2 && !mbar_wait(free_bar, (uint32_t)((item >> 1) & 1) ^ 1u, abort_flag)) fail(4);
-          const uint32_t to = sb + (which ? C::O_V : C::O_K) + buf * C::HALF_BYTES + tok * 128;
+          const int buf = which ? item & 1 : 0;
+          const uint32_t ready = which ? bar_vready + 8 * buf : bar_kready;
+          if (!mbar_wait(bar_in + 8 * (which * C::STAGES + stage), (uint32_t)((item / C::STAGES) & 1), abort_flag)) fail(3);
+          if (which == 0 && item > 0 && !mbar_wait(bar_kfree, (uint32_t)((item - 1) & 1), abort_flag)) fail(4);
+          if (which == 1 && item > 1 && !mbar_wait(bar_vfree + 8 * buf, (uint32_t)((item >> 1) & 1) ^ 1u, abort_flag)) fail(4);
+          const uint32_t to = sb + (which ? C::O_V + buf * C::HALF_BYTES : C::O_K) + tok * 128, row_in = sb + C::O_CODES + (2 * stage + which) * C::TILE_BYTES + tok * D;
 #pragma unroll
           for (int c = 0; c < D / 16; ++c) {
             const uint32_t ch = D == 64 ? c ^ ((tok >> 1) & 3) : c ^ (tok & 7);
-            const uint4 w = lds128(row_in + which * C::TILE_BYTES + ch * 16);
+            const uint4 w = lds128(row_in + ch * 16);
             // f16 order inside four: dimensions 0, 2, 1, 3
             const uint32_t at16 = to + (c >> 2) * (TK * 128), c0 = 2 * (c & 3);
             sts128(at16 + ((c0 ^ (tok & 7)) << 4), half_pair(w.x), half_pair(w.x >> 8), half_pair(w.y), half_pair(w.y >> 8));
@@ -282,7 +297,7 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(ready);
-            mbar_arrive(bar_read + 8 * which);
+            mbar_arrive(bar_read + 8 * (which * C::STAGES + stage));
           }
         }
       }
@@ -292,50 +307,60 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
     // ===================== MMAs =====================
     if (elect_one()) {
       constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);                              // rows of 128 bytes in the 128-byte swizzle
-      constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(TK >> 3) << 17) | (8u << 24);              // FP32 sums, f16 x f16
+      constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(C::STEP >> 3) << 17) | (8u << 24);         // FP32 sums, f16 x f16
       constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);  // B (values) dimension-major
       auto lo = [](uint32_t addr, uint32_t lead) { return (addr >> 4) | (lead << 16); };           // lead: from one 64-dimension block to the next
-      int item = 0, units = 0;
+      int tiles = 0, done = 0, units = 0;                          // tiles whose keys, values were waited for; steps of the units before
       bool alive = true;
       auto wait = [&](uint32_t b, int phase, uint32_t code) {
         if (alive && !mbar_wait(b, (uint32_t)(phase & 1), abort_flag)) { fail(code); alive = false; }
         return alive;
       };
-      auto products = [&](int i, int t, bool fresh) {              // O_t += P_t V of tile i
-        if (!wait(bar_p + 8 * t, i, 5) || (t == 0 && !wait(bar_vready + 8 * (i & 1), i >> 1, 6))) return;
-        tc_fence_after();
-        const uint32_t v = sb + C::O_V + (i & 1) * C::HALF_BYTES;
-#pragma unroll
-        for (int k = 0; k < TK / 16; ++k) mma_ts(tmem_o + 128 * t, tmem + 128 * t + 64 * (k / 4) + 8 * (k % 4), lo(v + k * 2048, TK * 128 / 16), hi, id_o, !fresh || k > 0);
-      };
       for (;;) {
         const Seg g = segment(at);
-        if (g.last > g.first) {
-          for (int j = g.first; alive && j < g.last; ++j, ++item) {
-            const int buf = item & 1;
-            if (!wait(bar_kready + 8 * buf, item >> 1, 7)) break;
-            for (int t = 0; t < 2 && alive; ++t) {
-              if (j > g.first) products(item - 1, t, j - 1 == g.first);
-              else wait(bar_q + 8 * t, units, 8);
-              if (!alive) break;
-              tc_fence_after();
-              const uint32_t k0 = sb + C::O_K + buf * C::HALF_BYTES, q0 = sb + C::O_Q + t * C::HALF_BYTES;
+        if (g.steps > 0) {
+          int k_tiles = tiles;
+          // scores of step n of the unit, both row tiles or one
+          auto scores = [&](int n, int t) {
+            const int b = (done + n) & 1;
+            const uint32_t k0 = sb + C::O_K + (n & 1) * (C::STEP * 128), q0 = sb + C::O_Q + t * C::HALF_BYTES, d = tmem + 128 * t + 64 * b;
 #pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k >> 2) * (TK * 128) + (k & 3) * 32;
-                mma_ss(tmem + 128 * t, lo(q0 + off, 1), lo(k0 + off, 1), hi, id_s, k > 0);
-              }
-              tc_commit(bar_s + 8 * t);
+            for (int k = 0; k < D / 16; ++k) {
+              const uint32_t off = (k >> 2) * (TK * 128) + (k & 3) * 32;
+              mma_ss(d, lo(q0 + off, 1), lo(k0 + off, 1), hi, id_s, k > 0);
             }
-            if (!alive) break;
-            tc_commit(bar_kfree + 8 * buf);
-            if (j > g.first) tc_commit(bar_vfree + 8 * (buf ^ 1));
+            tc_commit(bar_s + 16 * t + 8 * b);
+            if (t == 1 && ((n & 1) || n == g.steps - 1)) tc_commit(bar_kfree);
+          };
+          auto keys = [&](int n) { return (n & 1) || wait(bar_kready, k_tiles++, 7); };
+          for (int n = 0; n < 2 && n < g.steps && alive; ++n) {
+            if (!keys(n)) break;
+            for (int t = 0; t < 2 && alive; ++t) {
+              if (n == 0) wait(bar_q + 8 * t, units, 8);
+              tc_fence_after();
+              if (alive) scores(n, t);
+            }
           }
-          for (int t = 0; t < 2 && alive; ++t) {
-            products(item - 1, t, g.last - 1 == g.first);
-            if (alive) tc_commit(bar_o + 8 * t);
+          for (int n = 0; n < g.steps && alive; ++n) {
+            const int b = (done + n) & 1;
+            const int tile = tiles + (n >> 1);
+            if (!(n & 1) && !wait(bar_vready + 8 * (tile & 1), tile >> 1, 6)) break;
+            for (int t = 0; t < 2 && alive; ++t) {
+              if (!wait(bar_p + 16 * t + 8 * b, (done + n) >> 1, 5)) break;
+              tc_fence_after();
+              const uint32_t v = sb + C::O_V + (tile & 1) * C::HALF_BYTES + (n & 1) * (C::STEP * 128), pa = tmem + 128 * t + 64 * b;
+#pragma unroll
+              for (int k = 0; k < C::STEP / 16; ++k) mma_ts(tmem_o + 128 * t, pa + 8 * k, lo(v + k * 2048, TK * 128 / 16), hi, id_o, n > 0 || k > 0);
+              tc_commit(bar_o + 16 * t + 8 * b);
+              if (n + 2 < g.steps && (t > 0 || keys(n + 2))) {
+                tc_fence_after();
+                scores(n + 2, t);
+              }
+            }
+            if (alive && ((n & 1) || n == g.steps - 1)) tc_commit(bar_vfree + 8 * (tile & 1));
           }
-          if (alive) tc_commit(bar_vfree + 8 * ((item - 1) & 1));
+          tiles += g.last - g.first;
+          done += g.steps;
           ++units;
         }
         if (!alive || !walk_advance(a, TK, at, g.n_items)) break;
@@ -346,97 +371,112 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
     mbar_wait(bar_drain, 0, never);
     __syncwarp();
   } else if (warp < C::W_CODES) {
-    // ===================== softmax: two threads a row =====================
-    const int t = warp >> 3, half = (warp >> 2) & 1, row = 128 * t + 32 * (warp & 3) + lane;   // of the unit
-    float* top_mine = reinterpret_cast<float*>(sm + C::O_TOP) + (2 * t + half) * 128 + (row & 127);
-    const float* top_other = reinterpret_cast<float*>(sm + C::O_TOP) + (2 * t + (half ^ 1)) * 128 + (row & 127);
-    auto row_meet = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
-    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + lanes + 128 * t, t_o = tmem_o + lanes + 128 * t + half * (D / 2);
-    int item = 0, units = 0;
+    // ===================== softmax: a thread a row =====================
+    const int t = warp >> 2, row = 128 * t + 32 * (warp & 3) + lane;                  // of the unit
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + lanes + 128 * t, t_o = tmem_o + lanes + 128 * t;
+    // Where the threads are in the work lies in shared memory while they go through a unit: all registers are wanted there, and what spills comes
+    // from L2, since shared memory takes all of L1.
+    volatile Held* held = reinterpret_cast<volatile Held*>(misc + 16);
+    auto hold = [&]() {
+      threads_meet<C::SOFT>();                                                        // everyone has recalled the one before
+      if (threadIdx.x == 0) {
+        held->b = at.b, held->row0 = at.row0, held->n = at.n, held->len = at.len, held->tiles = at.tiles, held->units = at.units, held->unit = at.unit, held->tile = at.tile;
+        held->left = at.left, held->begin = begin, held->end = end, held->per = per;
+      }
+      threads_meet<C::SOFT>();
+    };
+    auto recall = [&]() {
+      at.b = held->b, at.row0 = held->row0, at.n = held->n, at.len = held->len, at.tiles = held->tiles, at.units = held->units, at.unit = held->unit, at.tile = held->tile;
+      at.left = held->left, begin = held->begin, end = held->end, per = held->per;
+    };
+    int tiles = 0, done = 0;                                                          // tiles, steps before the unit
     for (;;) {
-      const Seg g = segment(at);
-      const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
-      const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
-      const int see = real ? max(at.len - at.n + i + 1, 0) : 0x7FFFFFFF;
-      float m = -INFINITY, l = 0.0f, lg_ref = -INFINITY, f1 = 0.0f, f2 = 0.0f;
-      if (g.last > g.first) {
-        // ---- the row of queries, half of it a thread
-        uint32_t top = 0;
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + half * (D / 16);
+      hold();
+      float m = -INFINITY, l = 0.0f, lg_ref = -INFINITY;
+      int steps, see;
+      {
+        const Seg g = segment(at);
+        const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
+        const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
+        see = (real ? max(at.len - at.n + i + 1, 0) : 0x7FFFFFFF) - g.first * TK;      // keys from the segment's first on
+        steps = g.steps;
+      }
+      if (steps > 0) {
+        float f1, f2;
+        {
+          const Seg g = segment(at);
+          const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
+          const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
+          // ---- the row of queries
+          uint32_t top = 0;
+          const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          const uint4 x = real ? src[c] : make_uint4(0, 0, 0, 0);
-          top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
-        }
-        top = max(top >> 16, top & 0xFFFFu) << 16;
-        *top_mine = __uint_as_float(top);
-        row_meet();
-        top = max(top, __float_as_uint(*top_other));
-        row_meet();                                                                    // both have read
-        const bool bad = top >= 0x7F800000u || kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
-        const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
-        // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
-        const float up0 = (a.scale < 0.0f ? -1.0f : 1.0f) * power2((14 - e) / 2), up1 = power2(14 - e - (14 - e) / 2);
-        f1 = bad ? __uint_as_float(0x7FC00000u) : fabsf(a.scale) * LOG2E * power2(e / 2);
-        f2 = power2(e - e / 2 - 14);
-        const uint32_t to = sb + C::O_Q + t * C::HALF_BYTES + (row & 127) * 128;
-#pragma unroll
-        for (int c0 = 0; c0 < D / 16; ++c0) {
-          const int c = half * (D / 16) + c0;
-          const uint4 x = real && !bad ? src[c0] : make_uint4(0, 0, 0, 0);             // (again, from L1)
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {                                               // four dimensions, in the order 0, 2, 1, 3
-            const uint32_t p0 = k ? x.z : x.x, p1 = k ? x.w : x.y;
-            w[2 * k] = pack_half(__uint_as_float(p0 << 16) * up0 * up1, __uint_as_float(p1 << 16) * up0 * up1);
-            w[2 * k + 1] = pack_half(__uint_as_float(p0 & 0xFFFF0000u) * up0 * up1, __uint_as_float(p1 & 0xFFFF0000u) * up0 * up1);
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 x = real ? src[c] : make_uint4(0, 0, 0, 0);
+            top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
           }
-          sts128(to + (c >> 3) * (TK * 128) + (((c & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+          top = max(top >> 16, top & 0xFFFFu) << 16;
+          const bool bad = top >= 0x7F800000u || kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
+          const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
+          // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
+          const float up0 = (a.scale < 0.0f ? -1.0f : 1.0f) * power2((14 - e) / 2), up1 = power2(14 - e - (14 - e) / 2);
+          f1 = bad ? __uint_as_float(0x7FC00000u) : fabsf(a.scale) * LOG2E * power2(e / 2);
+          f2 = power2(e - e / 2 - 14);
+          const uint32_t to = sb + C::O_Q + t * C::HALF_BYTES + (row & 127) * 128;
+#pragma unroll 4
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 x = real && !bad ? src[c] : make_uint4(0, 0, 0, 0);            // (again, from L1)
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {                                             // four dimensions, in the order 0, 2, 1, 3
+              const uint32_t p0 = k ? x.z : x.x, p1 = k ? x.w : x.y;
+              w[2 * k] = pack_half(__uint_as_float(p0 << 16) * up0 * up1, __uint_as_float(p1 << 16) * up0 * up1);
+              w[2 * k + 1] = pack_half(__uint_as_float(p0 & 0xFFFF0000u) * up0 * up1, __uint_as_float(p1 & 0xFFFF0000u) * up0 * up1);
+            }
+            sts128(to + (c >> 3) * (TK * 128) + (((c & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_q + 8 * t);
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_q + 8 * t);
-        for (int j = g.first; j < g.last; ++j, ++item) {
-          const int tok0 = j * TK;
-          const bool edge = __any_sync(0xFFFFFFFFu, tok0 + TK > see);
-          if (!mbar_wait(bar_kready + 8 * (item & 1), (uint32_t)((item >> 1) & 1), abort_flag)) fail(9);   // the scales are in place
-          const float lg_top = meta_top[item & 3];
-          float c[4], lg[4];                                                           // of the half's four times sixteen columns
+#pragma unroll 1
+        for (int n = 0; n < steps; ++n) {
+          const int b = (done + n) & 1, tile = tiles + (n >> 1), tok = n * C::STEP;
+          const bool edge = __any_sync(0xFFFFFFFFu, tok + C::STEP > see);
+          if (!mbar_wait(bar_s + 16 * t + 8 * b, (uint32_t)((done + n) >> 1) & 1u, abort_flag)) fail(10);
+          __syncwarp();
+          tc_fence_after();
+          // The scales were put down before the tile's codes were asked for, and the scores came behind these.  (The barrier of the f16 keys is not for these
+          // threads to wait for: it may be two phases further by now, and a parity does not tell.)
+          const float lg_top = meta_top[tile % C::METAS];
+          float c[4], lg[4];                                                           // of the step's four times sixteen columns
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float2 sc = meta[(item & 3) * 8 + 4 * half + q];
+            const float2 sc = meta[tile % C::METAS * 8 + 4 * (n & 1) + q];
             c[q] = sc.x * f1;
             lg[q] = sc.y;
           }
-          const int first = tok0 + 64 * half;
-          if (!mbar_wait(bar_s + 8 * t, (uint32_t)(item & 1), abort_flag)) fail(10);
-          __syncwarp();
-          tc_fence_after();
-          // ---- the tile's maximum: of sixteen scores before their page's scale, which is not negative
+          // ---- the step's scores, and their maximum: of sixteen before their page's scale, which is not negative
+          uint32_t v[2][32];
+          tc_ld32(t_s + 64 * b, v[0]);
+          tc_ld32(t_s + 64 * b + 32, v[1]);
+          tc_wait_ld();
+          if (edge) {
+#pragma unroll
+            for (int x = 0; x < 64; ++x) v[x / 32][x % 32] = tok + x < see ? v[x / 32][x % 32] : 0xFF800000u;
+          }
           float most = -INFINITY;
-          bool usual = true;                                                           // factors of the scores that one FP32 number holds
+          bool usual = !edge;                                                          // and factors of the scores that one FP32 number holds
 #pragma unroll
-          for (int q = 0; q < 4; q += 2) {
-            uint32_t v[32];
-            tc_ld32(t_s + 64 * half + 16 * q, v);
-            if (edge) {
+          for (int q = 0; q < 4; ++q) {
+            float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = first + 16 * q + x < see ? v[x] : 0xFF800000u;
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-              for (int x = 0; x < 16; ++x) top[x & 1] = fmaxf(top[x & 1], __uint_as_float(v[16 * h + x]));
-              const float cf = c[q + h] * f2, topmost = fmaxf(top[0], top[1]);
-              usual = usual && (cf == 0.0f ? c[q + h] == 0.0f : fabsf(cf) > 1e-30f);
-              if (topmost > -INFINITY) most = fmaxf(most, topmost * c[q + h]);
-            }
+            for (int x = 0; x < 16; ++x) top[x & 1] = fmaxf(top[x & 1], __uint_as_float(v[q / 2][16 * (q & 1) + x]));
+            const float cf = c[q] * f2, topmost = fmaxf(top[0], top[1]);
+            usual = usual && (cf == 0.0f ? c[q] == 0.0f : fabsf(cf) > 1e-30f);
+            if (topmost > -INFINITY) most = fmaxf(most, topmost * c[q]);
           }
           most = most == -INFINITY ? most : most * f2;
-          *top_mine = most;
-          row_meet();                                  // (the next write comes behind the next S, which comes behind both halves' arrivals below)
-          most = fmaxf(most, *top_other);
           float fm = 1.0f;
           bool move = false;
           if (most > m + LAG) {                                                        // (or the first)
@@ -445,89 +485,101 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
             m = most;
             move = true;
           }
-          if (lg_top > lg_ref) {
-            fm *= ex2(lg_ref - lg_top);
-            lg_ref = lg_top;
+          if (lg_top > lg_ref) {                                                       // to twice the largest, so that a slightly larger one changes nothing
+            fm *= ex2(lg_ref - (lg_top + 1.0f));
+            lg_ref = lg_top + 1.0f;
             move = true;
           }
-          if (j > g.first && __any_sync(0xFFFFFFFFu, move)) {                         // (the last product with the values is over: S came behind it)
+          if (n > 0 && __any_sync(0xFFFFFFFFu, move)) {
+            // the last product with the values has to be over (the one before it is: these scores came behind it)
+            if (!mbar_wait(bar_o + 16 * t + 8 * (b ^ 1), (uint32_t)((done + n - 1) >> 1) & 1u, abort_flag)) fail(11);
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
-            for (int q = 0; q < D / 64; ++q) {
-              uint32_t v[32];
-              tc_ld32(t_o + 32 * q, v);
+            for (int q = 0; q < D / 16; ++q) {
+              uint32_t o[16];
+              tc_ld16(t_o + 16 * q, o);
+              tc_wait_ld();
+              uint32_t w[8];
 #pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * fm);
-              tc_st32(t_o + 32 * q, v);
+              for (int x = 0; x < 8; ++x) w[x] = __float_as_uint(__uint_as_float(o[x]) * fm);
+              tc_st8(t_o + 16 * q, w);
+#pragma unroll
+              for (int x = 0; x < 8; ++x) w[x] = __float_as_uint(__uint_as_float(o[8 + x]) * fm);
+              tc_st8(t_o + 16 * q + 8, w);
             }
           }
-          // ---- probabilities, each half's over its own scores: exp2(s cf - m), times the value scale of the page over the largest
+          // ---- probabilities, over the scores: exp2(s cf - m), times the value scale of the page over the reference
           const float m0 = m == -INFINITY ? 0.0f : m, lg0 = lg_ref == -INFINITY ? 0.0f : lg_ref;
-          if (!edge && __all_sync(0xFFFFFFFFu, usual)) {
+          if (__all_sync(0xFFFFFFFFu, usual)) {
             uint64_t sum = 0;                                                          // of even and odd columns
             const uint64_t minus_m = pair64(-m0, -m0);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              uint32_t v[16], p[8];
-              tc_ld16(t_s + 64 * half + 16 * q, v);
-              tc_wait_ld();
+              uint32_t p[8];
               const float cf = c[q] * f2, rel = ex2(lg[q] - lg0) * P_ONE;
               const uint64_t cf2 = pair64(cf, cf), rel2 = pair64(rel, rel);
 #pragma unroll
               for (int x = 0; x < 8; ++x) {
-                const uint64_t z = fma2(pair64(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), cf2, minus_m);
+                const uint64_t z = fma2(pair64(__uint_as_float(v[q / 2][16 * (q & 1) + 2 * x]), __uint_as_float(v[q / 2][16 * (q & 1) + 2 * x + 1])), cf2, minus_m);
                 const uint64_t e = pair64(ex2(low64(z)), ex2(high64(z)));
                 sum = add2(sum, e);
                 const uint64_t w = mul2(e, rel2);
                 p[x] = pack_half(low64(w), high64(w));
               }
-              tc_st8(t_s + 64 * half + 8 * q, p);
+              tc_st8(t_s + 64 * b + 8 * q, p);
             }
             l += low64(sum) + high64(sum);
           } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              uint32_t v[16], p[8];
-              tc_ld16(t_s + 64 * half + 16 * q, v);
-              tc_wait_ld();
+              uint32_t p[8];
               const float rel = ex2(lg[q] - lg0) * P_ONE;
 #pragma unroll
               for (int x = 0; x < 16; x += 2) {
                 float e[2], w[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                  const bool seen = first + 16 * q + x + k < see;                      // a scale that is NaN is not the hidden rows' affair
-                  e[k] = seen ? ex2(__fmaf_rn(__uint_as_float(v[x + k]) * c[q], f2, -m0)) : 0.0f;
+                  const bool seen = tok + 16 * q + x + k < see;                        // a scale that is NaN is not the hidden rows' affair
+                  e[k] = seen ? ex2(__fmaf_rn(__uint_as_float(v[q / 2][16 * (q & 1) + x + k]) * c[q], f2, -m0)) : 0.0f;
                   w[k] = seen ? e[k] * rel : 0.0f;
                 }
                 l += e[0] + e[1];
                 p[x / 2] = pack_half(w[0], w[1]);
               }
-              tc_st8(t_s + 64 * half + 8 * q, p);
+              tc_st8(t_s + 64 * b + 8 * q, p);
             }
           }
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p + 8 * t);
+          if (lane == 0) mbar_arrive(bar_p + 16 * t + 8 * b);
         }
-        if (!mbar_wait(bar_o + 8 * t, (uint32_t)(units & 1), abort_flag)) fail(11);
+        // The last product; those before it are over with it.  A barrier for each buffer: of one for all steps the phase before would not be known to be over,
+        // and a parity tells two neighbouring phases apart, no more.
+        if (!mbar_wait(bar_o + 16 * t + 8 * ((done + steps - 1) & 1), (uint32_t)((done + steps - 1) >> 1) & 1u, abort_flag)) fail(12);
         __syncwarp();
         tc_fence_after();
-        ++units;
-        *top_mine = l;
-        row_meet();
-        l += *top_other;
+        tiles += (steps + 1) >> 1;
+        done += steps;
       }
+      recall();
+      const Seg g = segment(at);
+      const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
+      const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
       // ---- the end of the unit.  lg_ref may be -infinity: nothing but values of scale 0 was met, and O is 0
-      const bool whole = g.first == 0 && g.n_items == at.tiles, any = g.last > g.first;
+      const bool whole = g.first == 0 && g.n_items == at.tiles, any = g.steps > 0;
       const float ta = lg_ref == -INFINITY ? -INFINITY : m + lg_ref;
       const long long out_row = (long long)(at.row0 + i) * a.c.heads * a.G + g.h * a.G + hq;
       float* part = a.parts + ((long long)blockIdx.x * 2 + (g.first > 0 ? 0 : 1)) * C::PART_FLOATS;
 #pragma unroll 1
-      for (int q = 0; q < D / 64; ++q) {
-        const int d0 = half * (D / 2) + 32 * q;
+      for (int q = 0; q < D / 32; ++q) {
+        const int d0 = 32 * q;
         uint32_t v[32];
-        if (any) tc_ld32(t_o + 32 * q, v);
+        if (any) {
+          tc_ld32(t_o + 32 * q, v);
+          tc_wait_ld();
+        }
 #pragma unroll
         for (int x = 0; x < 32; ++x) v[x] = any ? __float_as_uint(__uint_as_float(v[x]) * (1.0f / P_ONE)) : 0u;
         if (whole) {
@@ -543,12 +595,10 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
       }
       tc_fence_before();
       if (!whole) {
-        if (half == 0) {
-          __stcg(part + D * R + row, ta);
-          __stcg(part + D * R + R + row, m);
-          __stcg(part + D * R + 2 * R + row, l);
-        }
-        // the last of the unit's CTAs to get here adds the parts up, half a row a thread
+        __stcg(part + D * R + row, ta);
+        __stcg(part + D * R + R + row, m);
+        __stcg(part + D * R + 2 * R + row, l);
+        // the last of the unit's CTAs to get here adds the parts up, a thread a row
         const long long unit_begin = begin + (end - begin - at.left) - g.first;
         const int c_first = (int)(unit_begin / per), parts = (int)((unit_begin + at.tiles - 1) / per) - c_first + 1;
         threads_meet<C::SOFT>();
@@ -569,7 +619,7 @@ __global__ void __launch_bounds__(704, 1) attn_kv8_many_kernel(const __grid_cons
             top_m = nm;
           }
 #pragma unroll 1
-          for (int d = half * (D / 2); d < (half + 1) * (D / 2); d += 8) {
+          for (int d = 0; d < D; d += 8) {
             float sum[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) sum[x] = 0.0f;
