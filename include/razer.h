@@ -299,9 +299,9 @@ typedef struct razer_kv8 {
  * razer_kv8_append: writes the new tokens' keys and values, bf16 [T][heads][head_dim], k_stride and v_stride elements from one token
  * to the next (multiples of 8, so that columns of a wider matrix serve; 16-byte aligned).  For each page and head that gets
  * tokens, with s0 the scale so far (0 where the page's first token is new) and a the largest new magnitude: the scale becomes
- * s = max(s0, fl32(a / 127)) (2^-149 as in razer_quant_i8); where s > s0 > 0 the page's older codes become the nearest integers to
- * the exact code * s0 / s; the new codes are the nearest integers to the exact x / s.  A NaN or an infinity among the new values, or s0 NaN,
- * makes the page's scale NaN for that head (new codes 0, older codes as they were).  Codes behind the last token are left as they were.  Tokens whose
+ * s = max(s0, fl32(a / 127)) (2^-149 as in razer_quant_i8); where s > s0 > 0 the page's other codes become the nearest integers to
+ * the exact code * s0 / s, so that they keep their values; the new codes are the nearest integers to the exact x / s.  A NaN or an infinity among
+ * the new values, or s0 NaN, makes the page's scale NaN for that head (new codes 0, the others as they were).  Tokens whose
  * page the table does not name (an entry outside 0 .. pages - 1, or behind table_width) or whose position is negative (more new
  * tokens than kv_len) are not written.  A page that gets tokens belongs to one sequence; pages that sequences share must be full
  * ones. */

@@ -84,8 +84,8 @@ def append64(s, x, codes, scales):
                             codes[at, h, p] = 0
                         continue
                     step = max(s0, fresh)
-                    if step > s0 > 0:
-                        codes[at, h, :rows[0][1]] = np.rint(codes[at, h, :rows[0][1]].astype(np.float64) * float(s0) / float(step)).astype(np.int8)
+                    if step > s0 > 0:                        # the page's other codes keep their values
+                        codes[at, h] = np.rint(codes[at, h].astype(np.float64) * float(s0) / float(step)).astype(np.int8)
                     scales[at, h] = step
                     for (r, p), v in zip(rows, new):
                         codes[at, h, p] = np.clip(np.rint(v / float(step)), -127, 127).astype(np.int8) if step > 0 else 0
