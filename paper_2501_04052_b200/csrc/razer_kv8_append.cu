@@ -43,21 +43,20 @@ __global__ void __launch_bounds__(append_threads(D, PAGE)) kv8_append_kernel(con
   if (q.n == 0 || begin >= q.len) return;
   const int lo = max(first, (int)begin), hi = (int)min((long long)q.len, begin + PAGE);
   if (lo >= hi) return;
-  const int page = kv8_page(c, s, b, block);
-  if (page < 0) return;
-  int8_t* codes = (value ? c.v : c.k) + ((long long)page * c.heads + head) * PAGE * D;
-  float* scale = (value ? c.v_scales : c.k_scales) + (long long)page * c.heads + head;
+  const int page = kv8_page(c, s, b, block);                 // asked for, and looked at when the new values are on their way too
   const int r0 = lo - (int)begin, rows = hi - lo;            // rows of the page
   const long long stride = value ? v_stride : k_stride;
   const __nv_bfloat16* src = (value ? v_new : k_new) + (long long)(q.row0 + lo - first) * stride + (long long)head * D;
-  const float s0 = r0 > 0 ? *scale : 0.0f;
-
   uint4 x[VPT];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int i = tid + j * THREADS, r = i / VECS;
     x[j] = r < rows ? *reinterpret_cast<const uint4*>(src + (long long)r * stride + i % VECS * 8) : make_uint4(0, 0, 0, 0);
   }
+  if (page < 0) return;
+  int8_t* codes = (value ? c.v : c.k) + ((long long)page * c.heads + head) * PAGE * D;
+  float* scale = (value ? c.v_scales : c.k_scales) + (long long)page * c.heads + head;
+  const float s0 = r0 > 0 ? *scale : 0.0f;
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) top = bf16_pair_max(bf16_pair_max(bf16_pair_max(bf16_pair_max(top, x[j].x), x[j].y), x[j].z), x[j].w);
