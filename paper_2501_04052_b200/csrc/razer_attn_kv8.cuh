@@ -43,12 +43,14 @@ __device__ __forceinline__ float rebase(float m, float l, float top) { return m 
 // A place in a CTA's work: segments, each the part of one unit that falls to it.
 struct Walk {
   int b, row0, n, len, tiles, units, unit, tile;
+  bool over;                                             // longer than its table: its rows are NaN
   long long left;                                        // items that remain to the CTA
 };
 // Sequence b and its number of items.
 __device__ __forceinline__ long long walk_enter(const AttnArgs& a, int tokens, int b, Walk& w) {
   Kv8Seq q = kv8_seq(a.s, b);
-  if (kv8_over(a.c, a.s, q.len)) q.len = q.n;            // its rows will be NaN: a key for each, whatever page it is on
+  w.over = kv8_over(a.c, a.s, q.len);
+  if (w.over) q.len = q.n;                               // a key for each row, whatever page it is on
   w.b = b, w.row0 = q.row0, w.n = q.n, w.len = q.len;
   w.tiles = max((q.len + tokens - 1) / tokens, 1);
   w.units = (q.n + a.tq - 1) / a.tq * a.c.heads * a.chunks;
@@ -72,34 +74,44 @@ template <int THREADS>
 __device__ __forceinline__ bool attn_share(const AttnArgs& a, int tokens, int* words, long long* sums, long long& begin, long long& end, long long& per, Walk& at) {
   constexpr int WARPS = THREADS / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  long long total = 0;
-  for (int b = threadIdx.x; b < a.s.B; b += THREADS) total += walk_enter(a, tokens, b, at);
-  for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-  if (lane == 0) sums[warp] = total;
-  __syncthreads();
-  total = 0;
-  for (int w = 0; w < WARPS; ++w) total += sums[w];
-  per = (total + gridDim.x - 1) / gridDim.x;
-  begin = per * blockIdx.x;
-  end = min(begin + per, total);
-  if (begin >= end) return false;
+  const bool once = a.s.B <= THREADS;                    // every sequence has a thread: one look at it is enough
+  long long total = 0, mine = 0;
+  for (int b = threadIdx.x; b < a.s.B; b += THREADS) total += mine = walk_enter(a, tokens, b, at);
   long long base = 0;                                    // items of the sequences before this round's
+  if (!once) {
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    if (lane == 0) sums[warp] = total;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < WARPS; ++w) total += sums[w];
+  }
+#pragma unroll 1
   for (int b0 = 0;; b0 += THREADS) {
-    const int b = b0 + threadIdx.x;
-    const long long mine = b < a.s.B ? walk_enter(a, tokens, b, at) : 0;
+    if (!once) mine = b0 + (int)threadIdx.x < a.s.B ? walk_enter(a, tokens, b0 + threadIdx.x, at) : 0;
     long long upto = mine;
     for (int o = 1; o < 32; o <<= 1) {
       const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += v;
     }
-    __syncthreads();                                     // the sums of the round before have been read
+    if (!once) __syncthreads();                          // the sums of the round before have been read
     if (lane == 31) sums[warp] = upto;
     __syncthreads();
-    long long before = base;
-    for (int w = 0; w < warp; ++w) before += sums[w];
-    for (int w = 0; w < WARPS; ++w) base += sums[w];
+    long long before = base, all = 0;
+    for (int w = 0; w < WARPS; ++w) {
+      const long long v = sums[w];
+      if (w < warp) before += v;
+      all += v;
+    }
+    base += all;
+    if (once) total = all;
+    if (b0 == 0) {
+      per = (total + gridDim.x - 1) / gridDim.x;
+      begin = per * blockIdx.x;
+      end = min(begin + per, total);
+      if (begin >= end) return false;
+    }
     if (before + upto - mine <= begin && begin < before + upto) {
-      words[0] = b;
+      words[0] = b0 + threadIdx.x;
       *reinterpret_cast<long long*>(words + 2) = begin - (before + upto - mine);
     }
     if (base > begin) break;

@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       const int buf = n & 1;
       if (n >= 2 && !mbar_wait(bar_qempty + 8 * buf, (uint32_t)((n >> 1) & 1) ^ 1u, abort_flag)) { fail(2); break; }
       __syncwarp();
-      const bool over = kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
+      const bool over = at.over;
 #pragma unroll 1
       for (int c = 0; c < CHUNKS; ++c) {                          // eight rows at once, four lanes a row, D / 4 dimensions a lane
         const int j = lane >> 2, part = lane & 3, r = 8 * c + j, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
@@ -510,12 +510,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       for (int c = 0; c < CHUNKS; ++c) {
         if (has_dim) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = 8 * c + j;
-            float top = -INFINITY;
-            for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, stat[g * R + r]);
-            join[(group * 8 + j) * D + dim] = stat_a[r] == -INFINITY ? 0.0f : o[r] * ex2(stat_a[r] - top) * (1.0f / W_ONE);
-          }
+          for (int j = 0; j < 8; ++j) join[(group * 8 + j) * D + dim] = o[8 * c + j];
         }
         threads_meet<SOFT>();
         for (int x = threadIdx.x; x < 8 * (D / 4); x += SOFT) {
@@ -525,7 +520,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           for (int g = 0; g < GROUPS; ++g) ta = fmaxf(ta, stat[g * R + r]), tm = fmaxf(tm, stat[GROUPS * R + g * R + r]);
           for (int g = 0; g < GROUPS; ++g) {
             const float4 v = *reinterpret_cast<const float4*>(join + (g * 8 + j) * D + d);
-            sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+            const float f = stat[g * R + r] == -INFINITY ? 0.0f : ex2(stat[g * R + r] - ta) * (1.0f / W_ONE);
+            sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
             const float* q = stat + 2 * GROUPS * R + g * 4 * R + r;
             const float lg = q[0] + q[R] + q[2 * R] + q[3 * R];
             sum_l += rebase(stat[GROUPS * R + g * R + r], lg, tm) * lg;

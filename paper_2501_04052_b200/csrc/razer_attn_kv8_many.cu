@@ -48,6 +48,7 @@ struct ManyCfg {
 // A Walk and its run's bounds.
 struct Held {
   int b, row0, n, len, tiles, units, unit, tile;
+  bool over;
   long long left, begin, end, per;
 };
 
@@ -380,13 +381,13 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
     auto hold = [&]() {
       threads_meet<C::SOFT>();                                                        // everyone has recalled the one before
       if (threadIdx.x == 0) {
-        held->b = at.b, held->row0 = at.row0, held->n = at.n, held->len = at.len, held->tiles = at.tiles, held->units = at.units, held->unit = at.unit, held->tile = at.tile;
+        held->b = at.b, held->row0 = at.row0, held->n = at.n, held->len = at.len, held->tiles = at.tiles, held->units = at.units, held->unit = at.unit, held->tile = at.tile, held->over = at.over;
         held->left = at.left, held->begin = begin, held->end = end, held->per = per;
       }
       threads_meet<C::SOFT>();
     };
     auto recall = [&]() {
-      at.b = held->b, at.row0 = held->row0, at.n = held->n, at.len = held->len, at.tiles = held->tiles, at.units = held->units, at.unit = held->unit, at.tile = held->tile;
+      at.b = held->b, at.row0 = held->row0, at.n = held->n, at.len = held->len, at.tiles = held->tiles, at.units = held->units, at.unit = held->unit, at.tile = held->tile, at.over = held->over;
       at.left = held->left, begin = held->begin, end = held->end, per = held->per;
     };
     int tiles = 0, done = 0;                                                          // tiles, steps before the unit
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
           }
           top = max(top >> 16, top & 0xFFFFu) << 16;
-          const bool bad = top >= 0x7F800000u || kv8_over(a.c, a.s, __ldg(a.s.kv_len + at.b));
+          const bool bad = top >= 0x7F800000u || at.over;
           const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
           // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
           const float up0 = (a.scale < 0.0f ? -1.0f : 1.0f) * power2((14 - e) / 2), up1 = power2(14 - e - (14 - e) / 2);
