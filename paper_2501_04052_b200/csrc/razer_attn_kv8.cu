@@ -27,9 +27,12 @@ int launch_attn_kv8(const Kv8& c, const Kv8Batch& s, const void* q, long long q_
   a.q_stride = q_stride;
   a.scale = scale;
   a.G = q_heads / c.heads;
-  const long long rows = ((long long)s.T + s.B - 1) / s.B * a.G;       // of a sequence and key-value head, in the mean
-  static const int force = getenv("ATTN_MANY") ? atoi(getenv("ATTN_MANY")) : 33;   // XXX
-  if (rows >= force) return launch_attn_many(a, st);
+  // By the rows of queries that a sequence has for a key-value head, in the mean (which ones the device alone knows; either kernel takes any).  8 key-value
+  // heads x 8, 32 sequences of 4096 tokens, pages of 64, microseconds with few / many rows: 8 rows 58 / 216, 16 82 / 216, 32 169 / 218,
+  // 48 310 / 220 (the tile of 32 taken twice), 128 587 / 228.  RAZER_ATTN (environment, read once; a test aid): "few" or "many" takes that one.
+  static const char force = [] { const char* e = getenv("RAZER_ATTN"); return e ? e[0] : '\0'; }();
+  const long long rows = ((long long)s.T + s.B - 1) / s.B * a.G;
+  if (force == 'm' || (force != 'f' && rows > 32)) return launch_attn_many(a, st);
   return launch_attn_few(a, rows > 32 ? 32 : (int)rows, st);
 }
 

@@ -10,6 +10,9 @@ with A = sum p_j |v_j| / sum p_j and E = 2^-23 (D + 4) max S_abs + 2^-21:
    |lse - exact| <= E + 2^-22 |exact| + 2^-21
 """
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -400,3 +403,128 @@ def test_a_decode_step_as_it_is_used(b):
     assert ((y.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs()).all()
     s.k, s.v, s.ks, s.vs = (t.cpu() for t in s.dev)
     check_attn(b, s, q)
+
+
+@pytest.mark.parametrize("kernel", ["few", "many"])
+def test_attn_either_kernel_takes_any_batch(kernel):
+    """The attention's tests with all calls on one of its two kernels (the choice is read once a process)."""
+    here = os.path.abspath(__file__)
+    r = subprocess.run([sys.executable, "-m", "pytest", here, "-q", "-x", "-m", "gpu", "-k", "attn and not either_kernel and not beyond_32_bits"],
+                       env=dict(os.environ, RAZER_ATTN=kernel), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-1000:]
+
+
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 128)])
+def test_pools_beyond_32_bits(b, D, page):
+    """Pages whose bytes lie past 2^31 and 2^32: written and attended to like any other."""
+    H, pages = 8, (1 << 32) // (8 * page * D) + 300
+    pools = [torch.zeros((pages, H, page, D), dtype=torch.int8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros((pages, H), device="cuda") for _ in range(2)]
+    cache = b.make_kv8(*pools, *scales)
+    n = 5 * page + 3
+    places = torch.tensor([[pages - 1, 7, (1 << 31) // (H * page * D) + 1, pages - 200, 0, pages // 2]], dtype=torch.int32)
+    starts, lens = torch.tensor([0, n], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    g = torch.Generator().manual_seed(page)
+    k, v = (torch.randn((n, H, D), generator=g).bfloat16() for _ in range(2))
+    b.razer_kv8_append(cache, k.cuda(), v.cuda(), places.cuda(), starts, lens)
+    small = Batch([n], [n], H, D, page, seed=1)
+    small.table = torch.arange(6, dtype=torch.int32)[None, :]
+    small.pages = 6
+    small.k, small.v = (torch.zeros((6, H, page, D), dtype=torch.int8) for _ in range(2))
+    small.ks, small.vs = (torch.zeros((6, H)) for _ in range(2))
+    want = [append64(small, x, c, s) for x, c, s in ((k, small.k, small.ks), (v, small.v, small.vs))]
+    for i in range(2):
+        at = places[0].long().cuda()
+        assert np.array_equal(pools[i][at].cpu().numpy(), want[i][0]) and np.array_equal(scales[i][at].cpu().numpy(), want[i][1])
+        assert int((pools[i] != 0).sum()) == int((torch.from_numpy(want[i][0]) != 0).sum())      # nothing anywhere else
+    (small.k, small.ks), (small.v, small.vs) = ((torch.from_numpy(c), torch.from_numpy(s)) for c, s in want)
+    for rows in (1, n):                                      # few rows and many
+        q = torch.randn((rows, 2 * H, D), generator=g).bfloat16().cuda()
+        qs = torch.tensor([0, rows], dtype=torch.int32).cuda()
+        small.device(b)
+        got = b.razer_attn_kv8(cache, q, places.cuda(), qs, lens)
+        ref = b.razer_attn_kv8(small.cache, q, small.args[0], qs, lens)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_both_ways_into_the_library(b, monkeypatch, compiled):
+    """Plain calls through the compiled part of the binding and through ctypes, given and allocated outputs, and what each refuses."""
+    if compiled and b._call is None:
+        pytest.skip(b.call_route())
+    if not compiled:
+        monkeypatch.setattr(b, "_call", None)
+    s = Batch([3, 1], [40, 90], 2, 64, 16, seed=50)
+    q = queries(s, 4)
+    check_append(b, s, *fresh(s))
+    s.k, s.v, s.ks, s.vs = (x.cpu() for x in s.dev)
+    check_attn(b, s, q)
+    d = q.cuda()
+    for bad in (d.float(), d[:, :, ::2], d.transpose(0, 1), q):
+        with pytest.raises((AssertionError, RuntimeError)):
+            b.razer_attn_kv8(s.cache, bad, *s.args)
+    k = fresh(s)[0].cuda()
+    for args in ((k, k[:2], *s.args), (k[:, :1], k[:, :1], *s.args), (k, k, s.args[0].long(), *s.args[1:]), (k, k, s.args[0], s.args[1][:2], s.args[2]),
+                 (k, k, s.args[0].t(), *s.args[1:])):
+        with pytest.raises((AssertionError, RuntimeError)):
+            b.razer_kv8_append(s.cache, *args)
+    with pytest.raises(b.RazerError):
+        b.razer_attn_kv8(s.cache, d, *s.args, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    x = torch.randn((5, 64), generator=s.g).bfloat16().cuda()
+    codes, scales = b.razer_quant_i8(x)
+    mine = torch.empty_like(codes)
+    assert b.razer_quant_i8(x, mine)[0] is not None and torch.equal(mine, codes)
+    y = b.razer_gemm_i8(codes, scales, codes, scales)
+    out = torch.empty_like(y)
+    assert torch.equal(b.razer_gemm_i8(codes, scales, codes, scales, out), y) and torch.equal(out, y)
+    for args in ((codes, scales[:4], codes, scales), (codes[:, :48], scales, codes, scales), (codes.t(), scales, codes, scales), (codes, scales.double(), codes, scales)):
+        with pytest.raises((AssertionError, RuntimeError)):
+            b.razer_gemm_i8(*args)
+    with pytest.raises(b.RazerError):
+        b.razer_quant_i8(torch.zeros((2, 24), dtype=torch.bfloat16, device="cuda"))
+
+
+def test_two_streams_with_a_workspace_each(b):
+    """Two batches at once on two streams, many times; each as if it were alone."""
+    batches = [Batch([1] * 9, [900 + 31 * i for i in range(9)], 2, 64, 16, seed=60).device(b), Batch([70, 2], [1500, 333], 2, 128, 32, seed=61).device(b)]
+    qs = [queries(s, 4).cuda() for s in batches]
+    alone = [b.razer_attn_kv8(s.cache, q, *s.args) for s, q in zip(batches, qs)]
+    spaces = [b.alloc_attn_workspace(s.cache, 8, "cuda") for s in batches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    got = [[], []]
+    for _ in range(30):
+        for i, (s, q, st) in enumerate(zip(batches, qs, streams)):
+            with torch.cuda.stream(st):
+                got[i].append(b.razer_attn_kv8(s.cache, q, *s.args, workspace=spaces[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        b.razer_workspace_status(spaces[i])
+        assert all(torch.equal(o, alone[i][0]) and torch.equal(l, alone[i][1]) for o, l in got[i])
+
+
+def test_full_pages_may_be_shared(b):
+    """Two sequences over the same first pages (a common prompt)."""
+    s = Batch([1, 4], [70, 90], 2, 64, 16, seed=62)
+    s.table[1, :3] = s.table[0, :3]
+    check_attn(b, s, queries(s, 4))
+
+
+def test_rows_outside_the_buffers_count_as_none(b):
+    """q_start that leaves 0 .. T or falls: those sequences have no rows, the others are as ever."""
+    s = Batch([2, 3, 2], [20, 30, 40], 1, 64, 16, seed=63).device(b)
+    q = queries(s, 2).cuda()
+    ref, ref_lse = b.razer_attn_kv8(s.cache, q, *s.args)
+    for starts, fine in (([0, 2, 5, 9], [0, 1]), ([-1, 2, 5, 7], [1, 2]), ([0, 2, 1, 1], [0])):
+        st = torch.tensor(starts, dtype=torch.int32).cuda()
+        out, lse = torch.full_like(ref, 5.0), torch.full_like(ref_lse, 5.0)
+        ws = b.alloc_attn_workspace(s.cache, 2, "cuda")
+        b.razer_attn_kv8(s.cache, q, s.args[0], st, s.args[2], out=out, lse=lse, workspace=ws)
+        b.razer_workspace_status(ws)
+        for i in fine:
+            lo, hi = starts[i], starts[i + 1]
+            assert torch.equal(out[lo:hi], ref[lo:hi]) and torch.equal(lse[lo:hi], ref_lse[lo:hi]), starts
+        b.razer_kv8_append(s.cache, q[:, :1].contiguous(), q[:, :1].contiguous(), s.args[0], st, s.args[2])
+        torch.cuda.synchronize()
+        for t, keep in zip(s.dev, (s.k, s.v, s.ks, s.vs)):
+            t.copy_(keep)
