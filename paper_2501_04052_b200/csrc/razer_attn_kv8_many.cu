@@ -405,37 +405,53 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       if (steps > 0) {
         float f1, f2;
         {
+          // ---- the warp's 32 rows of queries, D / 8 lanes a row, sixteen bytes a lane (a thread a row by itself took 15000 cycles)
+          constexpr int LPR = D / 8, RPI = 32 / LPR;                                   // lanes a row, rows an iteration
           const Seg g = segment(at);
-          const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
-          const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
-          // ---- the row of queries
-          uint32_t top = 0;
-          const uint4* src = reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D);
+          const int piece = lane % LPR, r0 = 128 * t + 32 * (warp & 3);
+          int mine = 0;                                                                // exponent of the thread's own row; a large one where it is broken
+          auto fetch = [&](int it) {
+            const int r = r0 + it * RPI + lane / LPR, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
+            if (!(r < a.tq * a.Gc && i < at.n && hq < a.G)) return make_uint4(0, 0, 0, 0);
+            return *(reinterpret_cast<const uint4*>(a.q + (long long)(at.row0 + i) * a.q_stride + (long long)(g.h * a.G + hq) * D) + piece);
+          };
+          constexpr int AHEAD = 4;
+#pragma unroll 1
+          for (int it0 = 0; it0 < 32 / RPI; it0 += AHEAD) {
+            uint4 raw[AHEAD];
 #pragma unroll
-          for (int c = 0; c < D / 8; ++c) {
-            const uint4 x = real ? src[c] : make_uint4(0, 0, 0, 0);
-            top = __vmaxu2(__vmaxu2(top, __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu)), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+            for (int u = 0; u < AHEAD; ++u) raw[u] = fetch(it0 + u);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+              const uint4 x = raw[u];
+              uint32_t top = __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+              top = max(top >> 16, top & 0xFFFFu) << 16;
+#pragma unroll
+              for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+              const bool bad = top >= 0x7F800000u || at.over;
+              const int e = bad ? 1 << 20 : top > 0 ? ilogbf(__uint_as_float(top)) : 0, es = bad ? 0 : e;
+#pragma unroll
+              for (int k = 0; k < RPI; ++k) {
+                const int other = __shfl_sync(0xFFFFFFFFu, e, k * LPR);
+                if (lane == (it0 + u) * RPI + k) mine = other;
+              }
+              // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
+              const float up0 = bad ? 0.0f : (a.scale < 0.0f ? -1.0f : 1.0f) * power2((14 - es) / 2), up1 = power2(14 - es - (14 - es) / 2);
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {                                           // four dimensions, in the order 0, 2, 1, 3
+                const uint32_t p0 = bad ? 0u : k ? x.z : x.x, p1 = bad ? 0u : k ? x.w : x.y;
+                w[2 * k] = pack_half(__uint_as_float(p0 << 16) * up0 * up1, __uint_as_float(p1 << 16) * up0 * up1);
+                w[2 * k + 1] = pack_half(__uint_as_float(p0 & 0xFFFF0000u) * up0 * up1, __uint_as_float(p1 & 0xFFFF0000u) * up0 * up1);
+              }
+              const int r = 32 * (warp & 3) + (it0 + u) * RPI + lane / LPR;            // of the row tile
+              sts128(sb + C::O_Q + t * C::HALF_BYTES + r * 128 + (piece >> 3) * (TK * 128) + (((piece & 7) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
+            }
           }
-          top = max(top >> 16, top & 0xFFFFu) << 16;
-          const bool bad = top >= 0x7F800000u || at.over;
-          const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
-          // to [2^14, 2^15), turned round where the scale is negative, so that the largest score stays the largest
-          const float up0 = (a.scale < 0.0f ? -1.0f : 1.0f) * power2((14 - e) / 2), up1 = power2(14 - e - (14 - e) / 2);
+          const bool bad = mine == 1 << 20;
+          const int e = bad ? 0 : mine;
           f1 = bad ? __uint_as_float(0x7FC00000u) : fabsf(a.scale) * LOG2E * power2(e / 2);
           f2 = power2(e - e / 2 - 14);
-          const uint32_t to = sb + C::O_Q + t * C::HALF_BYTES + (row & 127) * 128;
-#pragma unroll 4
-          for (int c = 0; c < D / 8; ++c) {
-            const uint4 x = real && !bad ? src[c] : make_uint4(0, 0, 0, 0);            // (again, from L1)
-            uint32_t w[4];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {                                             // four dimensions, in the order 0, 2, 1, 3
-              const uint32_t p0 = k ? x.z : x.x, p1 = k ? x.w : x.y;
-              w[2 * k] = pack_half(__uint_as_float(p0 << 16) * up0 * up1, __uint_as_float(p1 << 16) * up0 * up1);
-              w[2 * k + 1] = pack_half(__uint_as_float(p0 & 0xFFFF0000u) * up0 * up1, __uint_as_float(p1 & 0xFFFF0000u) * up0 * up1);
-            }
-            sts128(to + (c >> 3) * (TK * 128) + (((c & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
-          }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_q + 8 * t);
@@ -572,33 +588,48 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       const bool whole = g.first == 0 && g.n_items == at.tiles, any = g.steps > 0;
       const float ta = lg_ref == -INFINITY ? -INFINITY : m + lg_ref;
       const long long out_row = (long long)(at.row0 + i) * a.c.heads * a.G + g.h * a.G + hq;
-      float* part = a.parts + ((long long)blockIdx.x * 2 + (g.first > 0 ? 0 : 1)) * C::PART_FLOATS;
-#pragma unroll 1
-      for (int q = 0; q < D / 32; ++q) {
-        const int d0 = 32 * q;
-        uint32_t v[32];
-        if (any) {
-          tc_ld32(t_o + 32 * q, v);
-          tc_wait_ld();
+      // sixteen columns of O, in the order of the dimensions 0, 2, 1, 3 of four, times f to the output
+      auto put = [&](int d, const float (&v)[16], float f, bool none) {
+        uint32_t w[8];
+#pragma unroll
+        for (int x = 0; x < 16; x += 4) {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(none ? 0.0f : v[x] * f, none ? 0.0f : v[x + 2] * f), hi = __floats2bfloat162_rn(none ? 0.0f : v[x + 1] * f, none ? 0.0f : v[x + 3] * f);
+          w[x / 2] = *reinterpret_cast<const uint32_t*>(&lo);
+          w[x / 2 + 1] = *reinterpret_cast<const uint32_t*>(&hi);
         }
-#pragma unroll
-        for (int x = 0; x < 32; ++x) v[x] = any ? __float_as_uint(__uint_as_float(v[x]) * (1.0f / P_ONE)) : 0u;
-        if (whole) {
-          if (real) {
-#pragma unroll
-            for (int x = 0; x < 32; x += 4)                                            // columns 0, 2, 1, 3 of four
-              attn_store<D>(a, out_row, d0 + x, make_float4(__uint_as_float(v[x]), __uint_as_float(v[x + 2]), __uint_as_float(v[x + 1]), __uint_as_float(v[x + 3])), l, ta, m);
+        uint4* to = reinterpret_cast<uint4*>(a.out + out_row * D + d);
+        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      };
+      float4* part = reinterpret_cast<float4*>(a.parts + ((long long)blockIdx.x * 2 + (g.first > 0 ? 0 : 1)) * C::PART_FLOATS);   // [D / 4][R] four columns, then the statistics
+      {
+        const bool none = l == 0.0f;
+        const float f = none || ta == -INFINITY ? 0.0f : ex2(ta - m) / l;
+        if (whole && real && a.lse) a.lse[out_row] = none ? -INFINITY : (m + log2f(l)) * LN2;
+#pragma unroll 2
+        for (int q = 0; q < D / 16; ++q) {
+          uint32_t o[16];
+          float v[16];
+          if (any) {
+            tc_ld16(t_o + 16 * q, o);
+            tc_wait_ld();
           }
-        } else {
 #pragma unroll
-          for (int x = 0; x < 32; ++x) __stcg(part + (d0 + x) * R + row, __uint_as_float(v[x]));
+          for (int x = 0; x < 16; ++x) v[x] = any ? __uint_as_float(o[x]) * (1.0f / P_ONE) : 0.0f;
+          if (whole) {
+            if (real) put(16 * q, v, f, none);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) __stcg(part + (4 * q + x) * R + row, make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]));
+          }
         }
       }
       tc_fence_before();
       if (!whole) {
-        __stcg(part + D * R + row, ta);
-        __stcg(part + D * R + R + row, m);
-        __stcg(part + D * R + 2 * R + row, l);
+        float* stat = reinterpret_cast<float*>(part) + D * R;
+        __stcg(stat + row, ta);
+        __stcg(stat + R + row, m);
+        __stcg(stat + 2 * R + row, l);
         // the last of the unit's CTAs to get here adds the parts up, a thread a row
         const long long unit_begin = begin + (end - begin - at.left) - g.first;
         const int c_first = (int)(unit_begin / per), parts = (int)((unit_begin + at.tiles - 1) / per) - c_first + 1;
@@ -611,30 +642,34 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         }
         threads_meet<C::SOFT>();
         if (misc[7]) {
-          auto at_part = [&](int c) { return a.parts + ((long long)(c_first + c) * 2 + (c == 0)) * C::PART_FLOATS + row; };
+          auto part_of = [&](int c) { return a.parts + ((long long)(c_first + c) * 2 + (c == 0)) * C::PART_FLOATS; };
           float top_a = -INFINITY, top_m = -INFINITY, sum_l = 0.0f;
+#pragma unroll 1
           for (int c = 0; c < parts; ++c) {
-            const float *p = at_part(c) + D * R, ac = __ldcg(p), mc = __ldcg(p + R), lc = __ldcg(p + 2 * R), nm = fmaxf(top_m, mc);
+            const float *p = part_of(c) + D * R + row, ac = __ldcg(p), mc = __ldcg(p + R), lc = __ldcg(p + 2 * R), nm = fmaxf(top_m, mc);
             top_a = fmaxf(top_a, ac);
             sum_l = rebase(top_m, sum_l, nm) * sum_l + rebase(mc, lc, nm) * lc;
             top_m = nm;
           }
+          const bool none = sum_l == 0.0f;
+          const float f = none || top_a == -INFINITY ? 0.0f : ex2(top_a - top_m) / sum_l;
+          if (real && a.lse) a.lse[out_row] = none ? -INFINITY : (top_m + log2f(sum_l)) * LN2;
 #pragma unroll 1
-          for (int d = 0; d < D; d += 8) {
-            float sum[8];
+          for (int d = 0; d < D; d += 16) {
+            float sum[16];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) sum[x] = 0.0f;
+            for (int x = 0; x < 16; ++x) sum[x] = 0.0f;
 #pragma unroll 2
             for (int c = 0; c < parts; ++c) {
-              const float* p = at_part(c);
-              const float ac = __ldcg(p + D * R), f = ac == -INFINITY ? 0.0f : ex2(ac - top_a);
+              const float* p = part_of(c);
+              const float ac = __ldcg(p + D * R + row), fc = ac == -INFINITY ? 0.0f : ex2(ac - top_a);
+              float4 v[4];
 #pragma unroll
-              for (int x = 0; x < 8; ++x) sum[x] += f * __ldcg(p + (d + x) * R);
+              for (int x = 0; x < 4; ++x) v[x] = __ldcg(reinterpret_cast<const float4*>(p) + (d / 4 + x) * R + row);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) sum[4 * x] += fc * v[x].x, sum[4 * x + 1] += fc * v[x].y, sum[4 * x + 2] += fc * v[x].z, sum[4 * x + 3] += fc * v[x].w;
             }
-            if (real) {
-              attn_store<D>(a, out_row, d, make_float4(sum[0], sum[2], sum[1], sum[3]), sum_l, top_a, top_m);
-              attn_store<D>(a, out_row, d + 4, make_float4(sum[4], sum[6], sum[5], sum[7]), sum_l, top_a, top_m);
-            }
+            if (real) put(d, sum, f, none);
           }
         }
         threads_meet<C::SOFT>();                                                           // misc[7] has been read
