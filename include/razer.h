@@ -269,10 +269,10 @@ int razer_quant_i8(const void* x_dev, int x_is_fp32, int M, int K, long long row
                    float* scales_dev, void* stream);
 
 /* Matrix product of 8-bit integers with a scale for each token and channel:
- * y[m][n] = bf16( fl32(x_scales[m] * w_scales[n]) * sum_k x_codes[m][k] * w_codes[n][k] ), the sum exact in 32 bits, any M >= 1
- * and N >= 1.  x_codes_dev int8 [M][K], w_codes_dev int8 [N][K] (16-byte aligned, any codes, -128 included), K a multiple of 16 up to
+ * y[m][n] = bf16( fl32(x_scales[m] * w_scales[n]) * sum_k x_codes[m][k] * w_codes[n][k] ), the sum exact in 32 bits,
+ * then FP32 (the sum rounded to 24 bits, their product to FP32), any M >= 1 and N >= 1.  x_codes_dev int8 [M][K], w_codes_dev int8 [N][K] (16-byte aligned, any codes, -128 included), K a multiple of 16 up to
  * 131056; y_dev bf16 [M][N].  Weights are taken as razer_quant_i8 writes them: no layout step and no workspace.  If a
- * device-side wait gives up (razer_workspace_status), the outputs concerned are NaN. */
+ * device-side wait gives up, the outputs concerned are NaN. */
 int razer_gemm_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev,
                   const float* w_scales_dev, int M, int N, int K, void* y_dev, void* stream);
 
@@ -315,9 +315,13 @@ int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_
  * the keys 0 .. p:
  *   s_j = scale * k_scale(page of j) * <q, k_code_j>,  out = sum_j exp(s_j) v_scale(page of j) v_code_j / sum_j exp(s_j)
  * out_dev: bf16 [T][q_heads][head_dim], 16-byte aligned; lse_dev: FP32 [T][q_heads], log sum_j exp(s_j), or NULL.  A row that
- * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN shows as NaN in the rows that see its page, and so does
- * a page that the table does not name; a sequence longer than the table gets NaN in all its rows.  Sums are FP32; query
- * rows and probabilities are rounded to f16 with a scale of their own (11 significant bits), keys and values exact.
+ * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN or negative shows as NaN in the rows that see its
+ * page, and so do a page that the table does not name and a NaN or an infinity among a row's queries; a sequence longer than the table
+ * gets NaN in all its rows.  Keys and values count exactly, sums are FP32.  What is rounded follows the kernel, and that the mean of the
+ * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head.  Up to 32 rows: queries to 2^-23 of their row's largest
+ * magnitude (24-bit fixed point: bf16 exactly down to 2^-14 of it), weights exp(s_j) v_scale to 2^-25 of the largest among 128
+ * consecutive keys.  More: both to f16, queries relative to their row's largest magnitude (bf16 exactly down to 2^-28 of it), weights
+ * with 11 significant bits or to 2^-30 of the row's largest exp(s_j) times the largest value scale among the pages.
  * The workspace is that of razer_attn_kv8_workspace_bytes, prepared once by razer_workspace_init; calls that may overlap on the
  * GPU must not share one (two replayed graphs included).  razer_workspace_status reports a wait that gave up. */
 int razer_attn_kv8_workspace_bytes(const razer_kv8* cache, int q_heads, size_t* bytes_out);

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       };
       auto step = [&]() {
         id = id_next;
-        ks = ks_next;
+        ks = ks_next < 0.0f ? __uint_as_float(0x7FC00000u) : ks_next;
         if (value) lg = vs_next >= 0.0f && vs_next < INFINITY ? log2f(vs_next) : __uint_as_float(0x7FC00000u);   // -infinity for 0
       };
       id_next = page_of(have + lane);

@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(append_threads(D, PAGE)) kv8_append_kernel(con
   const Kv8Seq q = kv8_seq(s, b);
   const int first = q.len - q.n, block = (max(first, 0) >> LOG2) + slot - ((q.row0 >> LOG2) + 2 * b);
   const long long begin = (long long)block << LOG2;
-  if (q.n == 0 || begin >= q.len) return;
+  if (q.n == 0 || block < 0 || begin >= q.len) return;     // (no block below 0 where q_start does not decrease)
   const int lo = max(first, (int)begin), hi = (int)min((long long)q.len, begin + PAGE);
   if (lo >= hi) return;
   const int page = kv8_page(c, s, b, block);                 // asked for, and looked at when the new values are on their way too

@@ -1,11 +1,13 @@
 """The paged 8-bit cache on the GPU: its writer bit for bit, and the attention over it against the definition in 64 bits.
 
-Bar of the attention.  Exact result o = sum p_j v_j / sum p_j.  What is rounded: the query row to f16 with a scale of its own (exact for bf16
-but for values below 2^-28 of the row's largest), scores and their exponents in FP32 (a score of magnitude S is off by at most (D + 4) 2^-24 S_abs with
-S_abs = scale * ks * sum_d |q_d k_d|; the tensor core's truncated additions are counted as 2^-23 each, and the exponential as 2^-21), weights
-p_j vs_j either to f16 (2^-11 of each, or 2^-39 of the largest) or to 24 bits of the largest among 128 tokens (2^-25 of that), sums in FP32, the result to bf16 (2^-8).
-A weight that is off by 2^-25 W, W = max p_j vs_j, moves the numerator by at most 2^-25 W |code| <= 2^-25 W 127, and n keys by n times that.  So
-with A = sum p_j |v_j| / sum p_j and E = 2^-23 (D + 4) max S_abs + 2^-21:
+Bar of the attention.  Exact result o = sum p_j v_j / sum p_j.  What is rounded: the query row to f16 or 24 bits with a scale of its own (exact
+for bf16 but for values below 2^-14 of the row's largest, which are off by at most 2^-23 of it), scores and their exponents in FP32 (a score of
+magnitude S is off by at most (D + 4) 2^-24 S_abs with S_abs = scale * ks * sum_d |q_d k_d|; the tensor core's truncated additions are counted as
+2^-23 each, and the exponential as 2^-21), weights p_j vs_j to 24 bits of the largest among 128 tokens (off by 2^-25 of that), or to f16 (off by
+2^-11 of each, or, where f16 has no more bits, by half its smallest step 2^-24; 2^6 stands for the row's largest p times twice the largest vs or more,
+so that this is at most 2^-30 max p max vs), sums in FP32, the result to bf16 (2^-8).
+A weight that is off by 2^-25 W, W = max(max_j p_j vs_j, 2^-5 max p max vs), moves the numerator by at most 2^-25 W |code| <= 2^-25 W 127, and n keys
+by n times that.  So with A = sum p_j |v_j| / sum p_j and E = 2^-23 (D + 4) max S_abs + 2^-21:
    |out - o| <= 2^-8 |o| + (2^-11 + 2 E + 2^-20) A + 2^-38 max |v| + 2^-25 127 n W / sum p_j
    |lse - exact| <= E + 2^-22 |exact| + 2^-21
 """
@@ -214,7 +216,10 @@ def check_attn(b, s, q, scale=None, workspace=None):
                 top = v.abs().max() if v.numel() else 0.0
                 e = 2.0 ** -23 * (s.D + 4) * room + 2.0 ** -21
                 sv = s.vs[s.table[i, :-(-s.total[i] // s.page)].long(), h].double().repeat_interleave(s.page)[:max(s.total[i], 0)]
-                most = (p * sv).max(dim=1, keepdim=True).values * 127 * (limit[:, None] + 1).clamp(min=0) if p.shape[1] else 0.0
+                most = 0.0
+                if p.shape[1]:
+                    most = torch.maximum((p * sv).max(dim=1, keepdim=True).values, 2.0 ** -5 * p.max(dim=1, keepdim=True).values * sv.max())
+                    most = most * 127 * (limit[:, None] + 1).clamp(min=0)
                 bar = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * e[:, None] + 2.0 ** -20) * size + 2.0 ** -38 * top + 2.0 ** -25 * most
                 off = (out[rows, h * G + gq] - want).abs()
                 assert (off <= bar).all(), (i, h, gq, float((off / bar.clamp(min=1e-300)).max()))
