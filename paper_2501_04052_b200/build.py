@@ -76,7 +76,7 @@ def build_call(verbose: bool = False) -> None:
         lib = os.path.join(root, "lib")
         ok, out = _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
                         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *("-I" + d for d in inc), CALL_SOURCE, "-o", path + ".tmp",
-                        "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + lib])
+                        "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", "-Wl,-rpath," + lib])
     except Exception as e:                               # no torch, or one that does not load
         ok, out = False, repr(e)
     if ok:

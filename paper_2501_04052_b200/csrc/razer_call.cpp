@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cmath>
 #include <torch/csrc/autograd/python_variable.h>
@@ -124,7 +125,7 @@ bool counts(const at::Tensor& t) {
 // The caller's tensor, or a new one where `o` is None; false where it is neither.
 bool given(PyObject* o, at::Tensor& t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
   if (o == Py_None) {
-    t = at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    t = at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));   // from the allocator, not through the dispatcher
     return true;
   }
   if (!plain(o)) return false;
