@@ -269,10 +269,10 @@ int razer_quant_i8(const void* x_dev, int x_is_fp32, int M, int K, long long row
                    float* scales_dev, void* stream);
 
 /* Matrix product of 8-bit integers with a scale for each token and channel:
- * y[m][n] = bf16( fl32(x_scales[m] * w_scales[n]) * sum_k x_codes[m][k] * w_codes[n][k] ), the sum exact in 32 bits,
- * then FP32 (the sum rounded to 24 bits, their product to FP32), any M >= 1 and N >= 1.  x_codes_dev int8 [M][K], w_codes_dev int8 [N][K] (16-byte aligned, any codes, -128 included), K a multiple of 16 up to
- * 131056; y_dev bf16 [M][N].  Weights are taken as razer_quant_i8 writes them: no layout step and no workspace.  If a
- * device-side wait gives up, the outputs concerned are NaN. */
+ * y[m][n] = bf16( fl32(x_scales[m] * w_scales[n]) * sum_k x_codes[m][k] * w_codes[n][k] ), the sum exact in 32 bits, then FP32
+ * (the sum rounded to 24 bits, the product once).  M and N from 1 to 2^31 - 256, K a multiple of 16 up to 131056.  x_codes_dev
+ * int8 [M][K], w_codes_dev int8 [N][K] (16-byte aligned, any codes, -128 included); y_dev bf16 [M][N].  Weights are taken as
+ * razer_quant_i8 writes them: no layout step and no workspace.  If a device-side wait gives up, the outputs concerned are NaN. */
 int razer_gemm_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev,
                   const float* w_scales_dev, int M, int N, int K, void* y_dev, void* stream);
 

@@ -452,6 +452,7 @@ int razer_quant_i8(const void* x_dev, int x_is_fp32, int M, int K, long long row
 int razer_gemm_i8(const int8_t* x_codes_dev, const float* x_scales_dev, const int8_t* w_codes_dev, const float* w_scales_dev, int M, int N, int K,
                   void* y_dev, void* stream) {
   if (M < 1 || N < 1 || K < 16 || K % 16) return set_error(RAZER_ERR_INVALID_ARG, "M=%d N=%d K=%d invalid (K %% 16 == 0)", M, N, K);
+  if (M > 0x7FFFFF00 || N > 0x7FFFFF00) return set_error(RAZER_ERR_UNSUPPORTED, "M=%d N=%d: at most 2^31 - 256", M, N);
   if (K > 131056) return set_error(RAZER_ERR_UNSUPPORTED, "K=%d: the sum would not fit 32 bits (K <= 131056)", K);
   RAZER_TRY(check_ptr(x_codes_dev, 16, "x_codes_dev"));
   RAZER_TRY(check_ptr(x_scales_dev, 4, "x_scales_dev"));

@@ -10,8 +10,9 @@
 // first tiles next to never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16
 // times 2^6 (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to
 // twice the largest met.
-// What bounds it: the exponentials (16 a cycle: 2048 cycles a tile of 256 x 128), the MMAs (2800, those of S half as wide as they are long), and the chain of one
-// step's softmax.
+// What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 376 us (704 TFLOP/s, 950 W): 6000 to 6900 cycles for 256 rows x 128
+// tokens.  Without the softmax they take 4500: the MMAs of S, half as wide as they are long, 1700, those of O 600, and the shared memory that these share with the
+// conversion of the codes (96 KB a tile).  The exponentials alone are 2048 (16 a cycle).
 // Row tiles of a sequence are taken in the order first, last, second, last but one ..., so that equal runs of them are about equal work under the
 // causal mask.  Work is cut among the CTAs as razer_attn_kv8.cuh says.
 #include "razer_attn_kv8.cuh"

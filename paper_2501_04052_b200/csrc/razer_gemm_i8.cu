@@ -6,6 +6,12 @@
 // MMAs, warps 2-5 store.  One output tile belongs to a cluster of 1, 2, 4 or 8 CTAs that share its K: with few tokens there are fewer
 // tiles than SMs, and every weight byte comes from HBM once whatever the split.  The parts meet in distributed shared memory - integers, so that their
 // order does not matter - and each CTA finishes 128 / split of the rows: no workspace, no counters, nothing left between calls.
+//
+// i8_pair_kernel: two CTAs on 256 weight rows x up to 256 tokens, for more tokens than a few dozen (below).
+//
+// What bounds them, in a graph (a host loop in brackets, where the power limit lowers the clock): 1 x 11008 x 4096 10.2 us (11.0), 16 x 28672 x 8192 38.8 (40.1,
+// 5.9 TB/s): the weights from HBM, and the launch; 333 x 4096 x 11008 17 (21): 64 pairs of CTAs that take in 1.9 MB a CTA at 150 GB/s;
+// 2048 x 14336 x 4096 80 (99, 2.4 POP/s): the MMAs, under the power limit.
 #include "razer_common.cuh"
 #include "razer_tcgen05.cuh"
 

@@ -208,3 +208,28 @@ def test_quantize_and_multiply_back_to_back(b, M):
         xc, xsc = (torch.from_numpy(a) for a in quantize64(xs[i % 4].double().cpu().numpy()))
         want = exact_product(xc, xsc, wc, wsc)
         assert ((got[i].double().cpu() - want).abs() <= BAR * want.abs()).all(), i
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 33000, 70000), (33000, 24, 70000), (46400, 46500, 16)])
+def test_gemm_i8_beyond_32_bits(b, M, N, K):
+    """Operands and a result of more than 2^31 elements: the last rows and columns, and the first, against 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x, w = (torch.randint(-128, 128, (r, K), generator=g, dtype=torch.int8, device="cuda") for r in (M, N))
+    sx, sw = torch.rand(M, generator=g, device="cuda") + 0.01, torch.rand(N, generator=g, device="cuda") + 0.01
+    y = b.razer_gemm_i8(x, sx, w, sw)
+    at = lambda n: torch.unique(torch.tensor([0, 1, 2, n // 2, n - 3, n - 2, n - 1], device="cuda").clamp(0, n - 1))  # noqa: E731
+    m, n = at(M), at(N)
+    want = exact_product(x[m], sx[m], w[n], sw[n])
+    assert ((y[m][:, n].double() - want).abs() <= BAR * want.abs()).all()
+
+
+def test_quant_i8_beyond_32_bits(b):
+    M, K = 33000, 70000
+    x = torch.full((M, K), 0.5, dtype=torch.bfloat16, device="cuda")
+    rows = [0, M // 2, M - 2, M - 1]
+    for r in rows:
+        x[r] = torch.randn(K, generator=torch.Generator().manual_seed(r)).bfloat16().cuda()
+    codes, scales = b.razer_quant_i8(x)
+    want_codes, want_scales = quantize64(x[rows].double().cpu().numpy())
+    assert np.array_equal(codes[rows].cpu().numpy(), want_codes) and np.array_equal(scales[rows].cpu().numpy(), want_scales)
+    assert (codes[1] == 127).all() and (codes[M - 3] == 127).all()

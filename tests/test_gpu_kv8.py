@@ -533,3 +533,39 @@ def test_rows_outside_the_buffers_count_as_none(b):
         torch.cuda.synchronize()
         for t, keep in zip(s.dev, (s.k, s.v, s.ks, s.vs)):
             t.copy_(keep)
+
+
+def test_a_captured_decode_step_replayed(b):
+    """The whole step in one graph, its inputs and lengths changed between replays, against the same calls one by one."""
+    hidden, H, G, D, page, steps = 256, 2, 4, 64, 16, 20
+    first = [1, 30, 200]
+    s = Batch([1] * 3, [t + steps for t in first], H, D, page, seed=50).device(b)
+    g = torch.Generator().manual_seed(51)
+    weights = b.razer_quant_i8((0.05 * torch.randn(((H * G + 2 * H) * D, hidden), generator=g)).cuda())
+    xs = torch.randn((steps, 3, hidden), generator=g).bfloat16().cuda()
+    table, starts = s.args[0], s.args[1]
+    x, lens = xs[0].clone(), torch.zeros(3, dtype=torch.int32, device="cuda")
+
+    def step(cache, ws):
+        qkv = b.razer_gemm_i8(*b.razer_quant_i8(x), *weights)
+        q = qkv[:, :H * G * D].unflatten(1, (H * G, D))
+        k = qkv[:, H * G * D:(H * G + H) * D].unflatten(1, (H, D))
+        v = qkv[:, (H * G + H) * D:].unflatten(1, (H, D))
+        b.razer_kv8_append(cache, k, v, table, starts, lens)
+        return b.razer_attn_kv8(cache, q, table, starts, lens, workspace=ws)
+
+    pools = [t.clone() for t in s.dev]
+    apart = b.make_kv8(*pools)
+    ws = [b.alloc_attn_workspace(s.cache, H * G, "cuda") for _ in range(2)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(s.cache, ws[0])
+    for i in range(steps):
+        x.copy_(xs[i])
+        lens.copy_(torch.tensor([t + i + 1 for t in first], dtype=torch.int32))
+        graph.replay()
+        want = step(apart, ws[1])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+    assert all(torch.equal(p, t) for p, t in zip(pools, s.dev))
+    for w in ws:
+        b.razer_workspace_status(w)

@@ -41,6 +41,8 @@ def test_quant_i8_refuses(b, args, code):
     ((AT, AT, AT, AT, 8, 0, 64, AT, None), "INVALID_ARG"),
     ((AT, AT, AT, AT, 8, 8, 40, AT, None), "INVALID_ARG"),
     ((AT, AT, AT, AT, 8, 8, 131072, AT, None), "UNSUPPORTED"),     # (-128)^2 * 131072 = 2^31
+    ((AT, AT, AT, AT, 0x7FFFFF01, 8, 64, AT, None), "UNSUPPORTED"),
+    ((AT, AT, AT, AT, 8, 0x7FFFFFFF, 64, AT, None), "UNSUPPORTED"),
     ((AT + 8, AT, AT, AT, 8, 8, 64, AT, None), "INVALID_ARG"),
     ((AT, AT + 2, AT, AT, 8, 8, 64, AT, None), "INVALID_ARG"),
     ((AT, AT, AT + 8, AT, 8, 8, 64, AT, None), "INVALID_ARG"),
