@@ -303,8 +303,8 @@ typedef struct razer_kv8 {
  * the exact code * s0 / s, so that they keep their values; the new codes are the nearest integers to the exact x / s.  A NaN or an infinity among
  * the new values, or s0 NaN, makes the page's scale NaN for that head (new codes 0, the others as they were).  Tokens whose
  * page the table does not name (an entry outside 0 .. pages - 1, or behind table_width) or whose position is negative (more new
- * tokens than kv_len) are not written.  A page that gets tokens belongs to one sequence; pages that sequences share must be full
- * ones. */
+ * tokens than kv_len) are not written.  A page that gets tokens belongs to one sequence and one place of its table; pages that
+ * sequences share must be full ones. */
 int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_stride, const void* v_new_dev,
                      long long v_stride, const int32_t* block_table_dev, int table_width,
                      const int32_t* q_start_dev, const int32_t* kv_len_dev, int B, int T, void* stream);

@@ -6,7 +6,7 @@ namespace razer {
 size_t attn_few_part_floats(int D);
 int launch_attn_few(AttnArgs& a, int rows, cudaStream_t st);
 size_t attn_many_part_floats(int D);
-int launch_attn_many(AttnArgs& a, cudaStream_t st);
+int launch_attn_many(AttnArgs& a, bool pairs, cudaStream_t st);
 
 size_t attn_kv8_workspace_bytes(int D) {
   const size_t few = attn_few_part_floats(D), many = attn_many_part_floats(D);
@@ -29,10 +29,14 @@ int launch_attn_kv8(const Kv8& c, const Kv8Batch& s, const void* q, long long q_
   a.G = q_heads / c.heads;
   // By the rows of queries that a sequence has for a key-value head, in the mean (which ones the device alone knows; either kernel takes any).  8 key-value
   // heads x 8, 32 sequences of 4096 tokens, pages of 64, microseconds with few / many rows: 8 rows 58 / 216, 16 82 / 216, 32 169 / 218,
-  // 48 310 / 220 (the tile of 32 taken twice), 128 587 / 228.  RAZER_ATTN (environment, read once; a test aid): "few" or "many" takes that one.
+  // 48 310 / 220 (the tile of 32 taken twice), 128 587 / 228.  Pairs of CTAs
+  // (heads of 128) from 1024 rows on where a row tile of 512 is at most 128 tokens, so that the causal mask wastes little of it, many rows / pairs: 3 ragged
+  // sequences of 8192 with 4 x 1000 rows 373 / 352, 8192 rows over 32768 tokens 1229 / 1085, 2400 rows over 4000 86 / 82, 1024 over 8192 82 / 80; 512 over
+  // 8192 71 / 73, 510 over 4096 72 / 84, 2048 tokens among themselves with one query head 108 / 117.  RAZER_ATTN (environment, read once; a test aid): "few",
+  // "many" or "pair" takes that one.
   static const char force = [] { const char* e = getenv("RAZER_ATTN"); return e ? e[0] : '\0'; }();
   const long long rows = ((long long)s.T + s.B - 1) / s.B * a.G;
-  if (force == 'm' || (force != 'f' && rows > 32)) return launch_attn_many(a, st);
+  if (force ? force != 'f' : rows > 32) return launch_attn_many(a, force ? force == 'p' : rows >= 1024 && a.G >= 4, st);
   return launch_attn_few(a, rows > 32 ? 32 : (int)rows, st);
 }
 

@@ -68,10 +68,11 @@ __device__ __forceinline__ bool walk_advance(const AttnArgs& a, int tokens, Walk
   while (w.units == 0);
   return true;
 }
-// The CTA's run of items [begin, end), `per` to a CTA, and the place where it begins; false if it has none.  All threads; `words`: four words, and
+// The run of items [begin, end) of the CTA or pair of CTAs `share` of `shares`, `per` to each, and the place where it begins; false if it has none.  All threads; `words`: four words, and
 // `sums` one long long a warp, of shared memory.
 template <int THREADS>
-__device__ __forceinline__ bool attn_share(const AttnArgs& a, int tokens, int* words, long long* sums, long long& begin, long long& end, long long& per, Walk& at) {
+__device__ __forceinline__ bool attn_share(const AttnArgs& a, int tokens, int* words, long long* sums, long long& begin, long long& end, long long& per, Walk& at,
+                                           int share, int shares) {
   constexpr int WARPS = THREADS / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool once = a.s.B <= THREADS;                    // every sequence has a thread: one look at it is enough
@@ -105,8 +106,8 @@ __device__ __forceinline__ bool attn_share(const AttnArgs& a, int tokens, int* w
     base += all;
     if (once) total = all;
     if (b0 == 0) {
-      per = (total + gridDim.x - 1) / gridDim.x;
-      begin = per * blockIdx.x;
+      per = (total + shares - 1) / shares;
+      begin = per * share;
       end = min(begin + per, total);
       if (begin >= end) return false;
     }
@@ -205,16 +206,17 @@ __device__ __forceinline__ void attn_combine(const AttnArgs& a, const Walk& at, 
   }
 }
 
-// A tensor map over a pool of codes: (dimension, token of the page, page and head), boxes of `rows` tokens.
-static inline int attn_encode_pool(CUtensorMap* map, const void* p, const Kv8& c, int rows) {
+// A tensor map over a pool of codes: (dimension, token of the page, page and head), boxes of `rows` tokens and `columns` (64 or 128) of their
+// dimensions.
+static inline int attn_encode_pool(CUtensorMap* map, const void* p, const Kv8& c, int rows, int columns) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return set_error(RAZER_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.page, (cuuint64_t)c.pages * c.heads};
   const cuuint64_t strides[2] = {(cuuint64_t)c.D, (cuuint64_t)c.D * c.page};
-  const cuuint32_t box[3] = {(cuuint32_t)c.D, (cuuint32_t)rows, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)columns, (cuuint32_t)rows, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         c.D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         columns == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return set_error(RAZER_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
   return RAZER_OK;

@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
   grid_dep_launch();
   long long begin, end, per;
   Walk at;
-  const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at);   // barriers inside
+  const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at, blockIdx.x, gridDim.x);   // barriers inside
   tc_fence_after();
   const uint32_t tmem = (uint32_t)misc[6];
   const int heads = a.c.heads * a.chunks;
@@ -592,8 +592,8 @@ int launch_as(AttnArgs& a, cudaStream_t st) {
   a.chunks = (a.G + a.Gc - 1) / a.Gc;
   a.tq = R / a.Gc;
   CUtensorMap map_k, map_v;
-  RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, a.c.page));
-  RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page));
+  RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, a.c.page, D));
+  RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page, D));
   static std::atomic<uint64_t> allowed{0};
   RAZER_TRY(allow_smem((const void*)attn_kv8_few_kernel<D, R>, C::SMEM_BYTES, allowed));
   return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R>, sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS, C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);

@@ -10,9 +10,13 @@
 // first tiles next to never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16
 // times 2^6 (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to
 // twice the largest met.
-// What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 376 us (704 TFLOP/s, 950 W): 6000 to 6900 cycles for 256 rows x 128
-// tokens.  Without the softmax they take 4500: the MMAs of S, half as wide as they are long, 1700, those of O 600, and the shared memory that these share with the
-// conversion of the codes (96 KB a tile).  The exponentials alone are 2048 (16 a cycle).
+// A pair of CTAs (cta_group::2) takes 512 rows: each converts half of the keys of a step and half of the values' dimensions, so that a tile is
+// converted once for both, and the MMAs read half as much of it from either's shared memory.
+// What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 352 us (751 TFLOP/s) by pairs, 373 without: 2300 to 2500 cycles
+// for 256 rows x 64 tokens.  Without the softmax a single CTA takes 2200 (the MMAs of S, half as wide as they are long, 860, those of O 300, and shared memory that these share
+// with the conversion, 48 KB), a pair 1600.  The exponentials alone are 1024 (16 a cycle); XU 39 %, ALU 36 %, tensor 35 % busy, issue slots 47 %: what is left is
+// the chain of a step (scores read, maximum, exponentials, probabilities stored, 1900 cycles), of which a scheduler has two to interleave.
+// A unit's ends (queries in, sums out, parts joined) are a tenth of the time.
 // Row tiles of a sequence are taken in the order first, last, second, last but one ..., so that equal runs of them are about equal work under the
 // causal mask.  Work is cut among the CTAs as razer_attn_kv8.cuh says.
 #include "razer_attn_kv8.cuh"
@@ -26,21 +30,26 @@ namespace {
 constexpr float P_ONE = 64.0f;                           // what a probability of 1 is held as
 constexpr float LAG = 8.0f;                              // how far (log2) a maximum may run ahead of the one that sums are relative to
 
-template <int D_>
+// CTAS: one, or a pair that goes through the tiles together, 256 rows each.
+template <int D_, int CTAS_>
 struct ManyCfg {
-  static constexpr int D = D_, R = 256, TK = 128;
+  static_assert(CTAS_ == 1 || D_ == 128, "a pair's CTA holds 64 of 128 dimensions of the values");
+  static constexpr int D = D_, CTAS = CTAS_, R = 256, TK = 128;
   static constexpr int SOFT = 256, THREADS = 448, W_CODES = 8, W_LOAD = 12, W_MMA = 13;   // warps 0-3, 4-7: softmax of a row tile each; 8-11: codes to f16
   static constexpr int STEP = 64;                                      // tokens of a step
-  static constexpr int HALF_BYTES = TK * D * 2, TILE_BYTES = TK * D;
+  static constexpr int HALF_BYTES = TK * D * 2;                        // queries of a row tile
+  static constexpr int K_ROWS = TK / CTAS, V_DIMS = D / CTAS;          // a CTA's part of a tile: 64 / CTAS keys of each step, and V_DIMS of the values' dimensions
+  static constexpr int PART_BYTES = HALF_BYTES / CTAS, TILE_BYTES = TK * D / CTAS;
+  static constexpr int KBUF = CTAS;                                    // f16 keys: a pair has the room for two, and its barriers take longer (2400 cycles a step with one)
   static constexpr int O_Q = 0;                                        // [tile][block][128 rows][128 bytes]
   static constexpr int O_K = 2 * HALF_BYTES;                           // [block][128 tokens][128 bytes]
-  static constexpr int O_V = O_K + HALF_BYTES;                         // two buffers: the next tile's are made while products still read the last one's
-  static constexpr int STAGES = 2;                                     // of codes: with one, a copy's latency was in every tile (194 us of 458 were that skeleton)
-  static constexpr int O_CODES = O_V + 2 * HALF_BYTES;                     // keys, values of each stage: [128 tokens][D]
-  static constexpr int METAS = 8;                                      // tiles whose scales are held: two on their way, up to three in work
+  static constexpr int O_V = O_K + KBUF * PART_BYTES;                         // two buffers: the next tile's are made while products still read the last one's
+  static constexpr int STAGES = 2 * CTAS;                                     // of codes: with one, a copy's latency was in every tile (194 us of 458 were that skeleton)
+  static constexpr int O_CODES = O_V + 2 * PART_BYTES;                     // keys, values of each stage: [K_ROWS][D], [128 tokens][V_DIMS]
+  static constexpr int METAS = 8;                                      // tiles whose scales are held: up to four on their way, three in work
   static constexpr int O_META = O_CODES + 2 * STAGES * TILE_BYTES;     // [METAS][8] {key scale, log2 of the value scale}, [METAS] the largest of the latter
   static constexpr int O_BAR = O_META + METAS * 68;
-  static constexpr int N_BAR = 4 * STAGES + 6 + 2 + 4 + 4 + 4 + 1;
+  static constexpr int N_BAR = 4 * STAGES + 8 + 2 + 4 + 4 + 4 + 1;
   static constexpr int O_MISC = O_BAR + 8 * N_BAR;
   static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
   static constexpr int PART_FLOATS = R * (D + 3);                      // [D][R] O, [R] ta, tm, sum
@@ -106,38 +115,58 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// f16 MMAs, A from shared memory or TMEM
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 ad, bd;\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "mov.b64 ad, {%1, %3};\n\t"
-      "mov.b64 bd, {%2, %3};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], ad, bd, %4, p;\n\t}" ::"r"(d),
-      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
-      : "memory");
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
+// Two warps that go through a part of their code in turn.
+__device__ __forceinline__ void take_turn(int barrier) { asm volatile("bar.sync %0, 64;" ::"r"(barrier) : "memory"); }
+__device__ __forceinline__ void give_turn(int barrier) { asm volatile("bar.arrive %0, 64;" ::"r"(barrier) : "memory"); }
+// f16 MMAs, A from shared memory or TMEM; of one CTA or by the first of a pair for both.
+template <bool PAIR>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+#define RAZER_MMA_SS(GROUP)                                   \
+  asm volatile(                                               \
+      "{\n\t.reg .pred p;\n\t.reg .b64 ad, bd;\n\t"           \
+      "setp.ne.b32 p, %5, 0;\n\t"                             \
+      "mov.b64 ad, {%1, %3};\n\t"                             \
+      "mov.b64 bd, {%2, %3};\n\t"                             \
+      "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], ad, bd, %4, p;\n\t}" ::"r"(d), \
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) \
+      : "memory")
+  if (PAIR) RAZER_MMA_SS("2");
+  else RAZER_MMA_SS("1");
+#undef RAZER_MMA_SS
+}
+template <bool PAIR>
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 bd;\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "mov.b64 bd, {%2, %3};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], bd, %4, p;\n\t}" ::"r"(d),
-      "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
-      : "memory");
+#define RAZER_MMA_TS(GROUP)                                   \
+  asm volatile(                                               \
+      "{\n\t.reg .pred p;\n\t.reg .b64 bd;\n\t"               \
+      "setp.ne.b32 p, %5, 0;\n\t"                             \
+      "mov.b64 bd, {%2, %3};\n\t"                             \
+      "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], [%1], bd, %4, p;\n\t}" ::"r"(d), \
+      "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)  \
+      : "memory")
+  if (PAIR) RAZER_MMA_TS("2");
+  else RAZER_MMA_TS("1");
+#undef RAZER_MMA_TS
 }
 
-template <int D>
+template <int D, int CTAS>
 __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                const __grid_constant__ AttnArgs a) {
-  using C = ManyCfg<D>;
+  using C = ManyCfg<D, CTAS>;
   constexpr int TK = C::TK, R = C::R;
+  constexpr bool PAIR = CTAS == 2;
+  const int rank = PAIR ? (int)cluster_rank() : 0, share = blockIdx.x / CTAS, shares = gridDim.x / CTAS;
   extern __shared__ uint8_t attn_smem[];
   uint8_t* sm = attn_smem + ((1024 - (smem_u32(attn_smem) & 1023)) & 1023);
   const uint32_t sb = smem_u32(sm);
   // codes of keys / values in and read; f16 buffers ready and free; queries ready; S, P; products with the values done
   const uint32_t bar = sb + C::O_BAR;
-  const uint32_t bar_in = bar, bar_read = bar_in + 16 * C::STAGES, bar_kready = bar_read + 16 * C::STAGES, bar_kfree = bar_kready + 8, bar_vready = bar_kfree + 8,
+  const uint32_t bar_in = bar, bar_read = bar_in + 16 * C::STAGES, bar_kready = bar_read + 16 * C::STAGES, bar_kfree = bar_kready + 16, bar_vready = bar_kfree + 16,
                  bar_vfree = bar_vready + 16, bar_q = bar_vfree + 16, bar_s = bar_q + 16, bar_p = bar_s + 32, bar_o = bar_p + 32, bar_drain = bar_o + 32;   // in, read: [keys, values][stage]; s, p, o: [row tile][buffer]
   int* misc = reinterpret_cast<int*>(sm + C::O_MISC);                    // abort, never set, share (4 words), TMEM, last; sums from word 16
   volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(misc);
@@ -151,18 +180,18 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       mbar_init(bar_in + 8 * i, 1);
       mbar_init(bar_read + 8 * i, 4);              // a warp arrives by one lane: 32 arrivals of a warp take their turns
     }
-    mbar_init(bar_kready, 4);
-    mbar_init(bar_kfree, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar_vready + 8 * i, 4);
+      mbar_init(bar_kready + 8 * i, PAIR && rank == 0 ? 5 : 4);      // the other CTA's four by one
+      mbar_init(bar_kfree + 8 * i, 1);
+      mbar_init(bar_vready + 8 * i, PAIR && rank == 0 ? 5 : 4);
       mbar_init(bar_vfree + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar_q + 8 * i, 4);
+      mbar_init(bar_q + 8 * i, 4 * CTAS);
       mbar_init(bar_s + 16 * i, 1);
       mbar_init(bar_s + 16 * i + 8, 1);
-      mbar_init(bar_p + 16 * i, 4);
-      mbar_init(bar_p + 16 * i + 8, 4);
+      mbar_init(bar_p + 16 * i, 4 * CTAS);
+      mbar_init(bar_p + 16 * i + 8, 4 * CTAS);
       mbar_init(bar_o + 16 * i, 1);
       mbar_init(bar_o + 16 * i + 8, 1);
     }
@@ -173,16 +202,30 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
   if (warp == C::W_MMA) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc + 6)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc + 6)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc + 6)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   grid_dep_wait();
   grid_dep_launch();
   long long begin, end, per;
   Walk at;
-  const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at);
+  const bool work = attn_share<C::THREADS>(a, TK, misc + 2, reinterpret_cast<long long*>(misc + 16), begin, end, per, at, share, shares);
+  if (PAIR) {                                                          // both CTAs' barriers are ready
+    __syncwarp();
+    cluster_meet();
+  }
   tc_fence_after();
+  // A barrier that the MMAs wait for is that of the first CTA.
+  auto tell = [&](uint32_t b) {
+    if (PAIR) peer_arrive(peer_addr(b, 0));
+    else mbar_arrive(b);
+  };
   const uint32_t tmem = (uint32_t)misc[6], tmem_o = tmem + 256;        // S and P: two buffers of 64 columns a row tile; O behind
   auto fail = [&](uint32_t code) {
     *abort_flag = 1;
@@ -208,6 +251,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
   } else if (warp == C::W_LOAD) {
     // ===================== pages, scales, codes =====================
     const int boxes = TK >> a.c.page_log2;                       // pages of a tile
+    const int k_rows = PAIR ? min(a.c.page, 32) : a.c.page, k_boxes = C::K_ROWS / k_rows;        // of the keys: a pair's CTA takes 32 of 64 tokens
     int item = 0, asked_v = 0;                                   // tiles whose keys, values were asked for
     bool alive = true;
     do {
@@ -247,21 +291,33 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         if (lane < 8) meta[item % C::METAS * 8 + lane] = make_float2(k1, v1);
         if (lane == 0) meta_top[item % C::METAS] = most;
         __syncwarp();
-        auto bring = [&](const CUtensorMap* map, int which) {
-          const uint32_t in = bar_in + 8 * (which * C::STAGES + stage);
-          if (lane == 0) mbar_expect_tx(in, (uint32_t)((live << a.c.page_log2) * D));
+        {
+          const uint32_t in = bar_in + 8 * stage;
+          // box `lane` of the keys: its first token, of the tile
+          const int tok = PAIR ? (lane * k_rows >> 5) * 64 + rank * 32 + ((lane * k_rows) & 31) : lane * k_rows;
+          const int of = tok >> a.c.page_log2, k_page = __shfl_sync(0xFFFFFFFFu, id, (block0 - have + of) & 31);
+          const bool mine = lane < k_boxes && of < live;
+          const int n = __popc(__ballot_sync(0xFFFFFFFFu, mine));
+          if (lane == 0) mbar_expect_tx(in, (uint32_t)(n * k_rows * D));
           __syncwarp();
-          if (lane < live)
-            tma_load_3d(sb + C::O_CODES + (2 * stage + which) * C::TILE_BYTES + (uint32_t)((lane << a.c.page_log2) * D), map, 0, 0, max(page, 0) * a.c.heads + g.h, in);
+          if (mine)
+            tma_load_3d(sb + C::O_CODES + 2 * stage * C::TILE_BYTES + (uint32_t)(lane * k_rows * D), &map_k, 0, tok & (a.c.page - 1), max(k_page, 0) * a.c.heads + g.h, in);
           __syncwarp();
-        };
-        bring(&map_k, 0);
+        }
         if (round > 0) {
           if (!mbar_wait(bar_read + 8 * (C::STAGES + stage), (uint32_t)(round & 1) ^ 1u, abort_flag)) fail(2), alive = false;
           alive = __all_sync(0xFFFFFFFFu, alive);
           if (!alive) { ++item; break; }
         }
-        bring(&map_v, 1);
+        {
+          const uint32_t in = bar_in + 8 * (C::STAGES + stage);
+          if (lane == 0) mbar_expect_tx(in, (uint32_t)((live << a.c.page_log2) * C::V_DIMS));
+          __syncwarp();
+          if (lane < live)
+            tma_load_3d(sb + C::O_CODES + (2 * stage + 1) * C::TILE_BYTES + (uint32_t)((lane << a.c.page_log2) * C::V_DIMS), &map_v, rank * C::V_DIMS, 0,
+                        max(page, 0) * a.c.heads + g.h, in);
+          __syncwarp();
+        }
         ++asked_v;
       }
       if (!alive) break;
@@ -280,20 +336,25 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         const int stage = item % C::STAGES;
 #pragma unroll 1
         for (int which = 0; which < 2; ++which) {
-          const int buf = which ? item & 1 : 0;
-          const uint32_t ready = which ? bar_vready + 8 * buf : bar_kready;
+          const int buf = which ? item & 1 : item % C::KBUF;
+          const uint32_t ready = (which ? bar_vready : bar_kready) + 8 * buf;
           if (!mbar_wait(bar_in + 8 * (which * C::STAGES + stage), (uint32_t)((item / C::STAGES) & 1), abort_flag)) fail(3);
-          if (which == 0 && item > 0 && !mbar_wait(bar_kfree, (uint32_t)((item - 1) & 1), abort_flag)) fail(4);
+          if (which == 0 && item >= C::KBUF && !mbar_wait(bar_kfree + 8 * buf, (uint32_t)((item / C::KBUF) & 1) ^ 1u, abort_flag)) fail(4);
           if (which == 1 && item > 1 && !mbar_wait(bar_vfree + 8 * buf, (uint32_t)((item >> 1) & 1) ^ 1u, abort_flag)) fail(4);
-          const uint32_t to = sb + (which ? C::O_V + buf * C::HALF_BYTES : C::O_K) + tok * 128, row_in = sb + C::O_CODES + (2 * stage + which) * C::TILE_BYTES + tok * D;
+          // a thread's part: a token's row, or, of a pair's half as many keys, half of it
+          const bool split = PAIR && which == 0;
+          const int r = split ? tok & (C::K_ROWS - 1) : tok, c0 = split ? (tok / C::K_ROWS) * (D / 32) : 0, columns = which ? C::V_DIMS : D;
+          const uint32_t to = sb + (which ? C::O_V : C::O_K) + buf * C::PART_BYTES + r * 128, row_in = sb + C::O_CODES + (2 * stage + which) * C::TILE_BYTES + r * columns;
+          const uint32_t block = which ? TK * 128 : C::K_ROWS * 128;
 #pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint32_t ch = D == 64 ? c ^ ((tok >> 1) & 3) : c ^ (tok & 7);
+          for (int i = 0; i < C::V_DIMS / 16; ++i) {
+            const int c = c0 + i;
+            const uint32_t ch = columns == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7);
             const uint4 w = lds128(row_in + ch * 16);
             // f16 order inside four: dimensions 0, 2, 1, 3
-            const uint32_t at16 = to + (c >> 2) * (TK * 128), c0 = 2 * (c & 3);
-            sts128(at16 + ((c0 ^ (tok & 7)) << 4), half_pair(w.x), half_pair(w.x >> 8), half_pair(w.y), half_pair(w.y >> 8));
-            sts128(at16 + (((c0 + 1) ^ (tok & 7)) << 4), half_pair(w.z), half_pair(w.z >> 8), half_pair(w.w), half_pair(w.w >> 8));
+            const uint32_t at16 = to + (c >> 2) * block, h0 = 2 * (c & 3);
+            sts128(at16 + ((h0 ^ (r & 7)) << 4), half_pair(w.x), half_pair(w.x >> 8), half_pair(w.y), half_pair(w.y >> 8));
+            sts128(at16 + (((h0 + 1) ^ (r & 7)) << 4), half_pair(w.z), half_pair(w.z >> 8), half_pair(w.w), half_pair(w.w >> 8));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -305,17 +366,21 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       }
       if (!walk_advance(a, TK, at, g.n_items)) break;
     } while (!*abort_flag);
-  } else if (warp == C::W_MMA) {
+  } else if (warp == C::W_MMA && rank == 0) {
     // ===================== MMAs =====================
     if (elect_one()) {
       constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);                              // rows of 128 bytes in the 128-byte swizzle
-      constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(C::STEP >> 3) << 17) | (8u << 24);         // FP32 sums, f16 x f16
-      constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);  // B (values) dimension-major
+      constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(C::STEP >> 3) << 17) | ((8u * CTAS) << 24);         // FP32 sums, f16 x f16
+      constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((8u * CTAS) << 24);  // B (values) dimension-major
       auto lo = [](uint32_t addr, uint32_t lead) { return (addr >> 4) | (lead << 16); };           // lead: from one 64-dimension block to the next
+      auto commit = [&](uint32_t b) {                              // to this barrier of both CTAs
+        if (PAIR) commit_pair(b, 3u);
+        else tc_commit(b);
+      };
       int tiles = 0, done = 0, units = 0;                          // tiles whose keys, values were waited for; steps of the units before
       bool alive = true;
       auto wait = [&](uint32_t b, int phase, uint32_t code) {
-        if (alive && !mbar_wait(b, (uint32_t)(phase & 1), abort_flag)) { fail(code); alive = false; }
+        if (alive && !mbar_wait<PAIR>(b, (uint32_t)(phase & 1), abort_flag)) { fail(code); alive = false; }
         return alive;
       };
       for (;;) {
@@ -325,16 +390,20 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           // scores of step n of the unit, both row tiles or one
           auto scores = [&](int n, int t) {
             const int b = (done + n) & 1;
-            const uint32_t k0 = sb + C::O_K + (n & 1) * (C::STEP * 128), q0 = sb + C::O_Q + t * C::HALF_BYTES, d = tmem + 128 * t + 64 * b;
+            const int buf = (tiles + (n >> 1)) % C::KBUF;
+            const uint32_t k0 = sb + C::O_K + buf * C::PART_BYTES + (n & 1) * (C::STEP / CTAS * 128), q0 = sb + C::O_Q + t * C::HALF_BYTES, d = tmem + 128 * t + 64 * b;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (k >> 2) * (TK * 128) + (k & 3) * 32;
-              mma_ss(d, lo(q0 + off, 1), lo(k0 + off, 1), hi, id_s, k > 0);
+              mma_ss<PAIR>(d, lo(q0 + (k >> 2) * (TK * 128) + (k & 3) * 32, 1), lo(k0 + (k >> 2) * (C::K_ROWS * 128) + (k & 3) * 32, 1), hi, id_s, k > 0);
             }
-            tc_commit(bar_s + 16 * t + 8 * b);
-            if (t == 1 && ((n & 1) || n == g.steps - 1)) tc_commit(bar_kfree);
+            commit(bar_s + 16 * t + 8 * b);
+            if (t == 1 && ((n & 1) || n == g.steps - 1)) commit(bar_kfree + 8 * buf);
           };
-          auto keys = [&](int n) { return (n & 1) || wait(bar_kready, k_tiles++, 7); };
+          auto keys = [&](int n) {
+            if (n & 1) return true;
+            const int tile = k_tiles++;
+            return wait(bar_kready + 8 * (tile % C::KBUF), tile / C::KBUF, 7);
+          };
           for (int n = 0; n < 2 && n < g.steps && alive; ++n) {
             if (!keys(n)) break;
             for (int t = 0; t < 2 && alive; ++t) {
@@ -350,16 +419,16 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             for (int t = 0; t < 2 && alive; ++t) {
               if (!wait(bar_p + 16 * t + 8 * b, (done + n) >> 1, 5)) break;
               tc_fence_after();
-              const uint32_t v = sb + C::O_V + (tile & 1) * C::HALF_BYTES + (n & 1) * (C::STEP * 128), pa = tmem + 128 * t + 64 * b;
+              const uint32_t v = sb + C::O_V + (tile & 1) * C::PART_BYTES + (n & 1) * (C::STEP * 128), pa = tmem + 128 * t + 64 * b;
 #pragma unroll
-              for (int k = 0; k < C::STEP / 16; ++k) mma_ts(tmem_o + 128 * t, pa + 8 * k, lo(v + k * 2048, TK * 128 / 16), hi, id_o, n > 0 || k > 0);
-              tc_commit(bar_o + 16 * t + 8 * b);
+              for (int k = 0; k < C::STEP / 16; ++k) mma_ts<PAIR>(tmem_o + 128 * t, pa + 8 * k, lo(v + k * 2048, TK * 128 / 16), hi, id_o, n > 0 || k > 0);
+              commit(bar_o + 16 * t + 8 * b);
               if (n + 2 < g.steps && (t > 0 || keys(n + 2))) {
                 tc_fence_after();
                 scores(n + 2, t);
               }
             }
-            if (alive && ((n & 1) || n == g.steps - 1)) tc_commit(bar_vfree + 8 * (tile & 1));
+            if (alive && ((n & 1) || n == g.steps - 1)) commit(bar_vfree + 8 * (tile & 1));
           }
           tiles += g.last - g.first;
           done += g.steps;
@@ -367,14 +436,34 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         }
         if (!alive || !walk_advance(a, TK, at, g.n_items)) break;
       }
-      tc_commit(bar_drain);
+      if (PAIR) commit_pair(bar_drain, 1u);
+      else tc_commit(bar_drain);
     }
     __syncwarp();
     mbar_wait(bar_drain, 0, never);
     __syncwarp();
+  } else if (warp == C::W_MMA) {
+    // ===================== the second CTA's f16 keys and values, told to the first =====================
+    // (By this warp, not by the four that make them: a release of the cluster takes 900 cycles, and two of them a tile were 1700 cycles a step.)
+    if (elect_one()) {
+      int item = 0;
+      bool alive = true;
+      do {
+        const Seg g = segment(at);
+        for (int t = g.first; alive && t < g.last; ++t, ++item)
+          for (int which = 0; alive && which < 2; ++which) {
+            const uint32_t ready = (which ? bar_vready : bar_kready) + 8 * (item & 1);
+            alive = mbar_wait(ready, (uint32_t)((item >> 1) & 1), abort_flag);
+            if (alive) peer_arrive(peer_addr(ready, 0));
+            else fail(9);
+          }
+        if (!walk_advance(a, TK, at, g.n_items)) break;
+      } while (alive);
+    }
+    __syncwarp();
   } else if (warp < C::W_CODES) {
     // ===================== softmax: a thread a row =====================
-    const int t = warp >> 2, row = 128 * t + 32 * (warp & 3) + lane;                  // of the unit
+    const int t = warp >> 2, row = 128 * t + 32 * (warp & 3) + lane, urow = rank * R + row;   // of the CTA; of the unit
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, t_s = tmem + lanes + 128 * t, t_o = tmem_o + lanes + 128 * t;
     // Where the threads are in the work lies in shared memory while they go through a unit: all registers are wanted there, and what spills comes
     // from L2, since shared memory takes all of L1.
@@ -398,8 +487,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       int steps, see;
       {
         const Seg g = segment(at);
-        const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
-        const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
+        const int i = g.qt * a.tq + urow / a.Gc, hq = g.chunk * a.Gc + urow % a.Gc;
+        const bool real = urow < a.tq * a.Gc && i < at.n && hq < a.G;
         see = (real ? max(at.len - at.n + i + 1, 0) : 0x7FFFFFFF) - g.first * TK;      // keys from the segment's first on
         steps = g.steps;
       }
@@ -409,7 +498,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           // ---- the warp's 32 rows of queries, D / 8 lanes a row, sixteen bytes a lane (a thread a row by itself took 15000 cycles)
           constexpr int LPR = D / 8, RPI = 32 / LPR;                                   // lanes a row, rows an iteration
           const Seg g = segment(at);
-          const int piece = lane % LPR, r0 = 128 * t + 32 * (warp & 3);
+          const int piece = lane % LPR, r0 = rank * R + 128 * t + 32 * (warp & 3);
           int mine = 0;                                                                // exponent of the thread's own row; a large one where it is broken
           auto fetch = [&](int it) {
             const int r = r0 + it * RPI + lane / LPR, i = g.qt * a.tq + r / a.Gc, hq = g.chunk * a.Gc + r % a.Gc;
@@ -455,7 +544,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           f2 = power2(e - e / 2 - 14);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_q + 8 * t);
+          if (lane == 0) tell(bar_q + 8 * t);
         }
 #pragma unroll 1
         for (int n = 0; n < steps; ++n) {
@@ -489,7 +578,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           for (int q = 0; q < 4; ++q) {
             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int x = 0; x < 16; ++x) top[x & 1] = fmaxf(top[x & 1], __uint_as_float(v[q / 2][16 * (q & 1) + x]));
+            for (int x = 0; x < 16; x += 2) top[(x >> 1) & 1] = max3(top[(x >> 1) & 1], __uint_as_float(v[q / 2][16 * (q & 1) + x]), __uint_as_float(v[q / 2][16 * (q & 1) + x + 1]));
             const float cf = c[q] * f2, topmost = fmaxf(top[0], top[1]);
             usual = usual && (cf == 0.0f ? c[q] == 0.0f : fabsf(cf) > 1e-30f);
             if (topmost > -INFINITY) most = fmaxf(most, topmost * c[q]);
@@ -527,6 +616,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
               tc_st8(t_o + 16 * q + 8, w);
             }
           }
+          // The two row tiles' warps of a scheduler take turns with the exponentials: by themselves they go in step in a pair, 1450 cycles for what takes 1000 (388 -> 366 us).
+          if (PAIR && (t == 1 || n > 0)) take_turn(2 + 4 * t + (warp & 3));
           // ---- probabilities, over the scores: exp2(s cf - m), times the value scale of the page over the reference
           const float m0 = m == -INFINITY ? 0.0f : m, lg0 = lg_ref == -INFINITY ? 0.0f : lg_ref;
           if (__all_sync(0xFFFFFFFFu, usual)) {
@@ -568,10 +659,15 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
               tc_st8(t_s + 64 * b + 8 * q, p);
             }
           }
+          if (PAIR && (t == 0 || n < steps - 1)) give_turn(2 + 4 * (t ^ 1) + (warp & 3));
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p + 16 * t + 8 * b);
+          if (lane == 0) {
+            // what it tells of is in TMEM and ordered by the fence; a release of the cluster takes 900 cycles
+            if (PAIR) peer_arrive_relaxed(peer_addr(bar_p + 16 * t + 8 * b, 0));
+            else mbar_arrive(bar_p + 16 * t + 8 * b);
+          }
         }
         // The last product; those before it are over with it.  A barrier for each buffer: of one for all steps the phase before would not be known to be over,
         // and a parity tells two neighbouring phases apart, no more.
@@ -583,8 +679,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
       }
       recall();
       const Seg g = segment(at);
-      const int i = g.qt * a.tq + row / a.Gc, hq = g.chunk * a.Gc + row % a.Gc;
-      const bool real = row < a.tq * a.Gc && i < at.n && hq < a.G;
+      const int i = g.qt * a.tq + urow / a.Gc, hq = g.chunk * a.Gc + urow % a.Gc;
+      const bool real = urow < a.tq * a.Gc && i < at.n && hq < a.G;
       // ---- the end of the unit.  lg_ref may be -infinity: nothing but values of scale 0 was met, and O is 0
       const bool whole = g.first == 0 && g.n_items == at.tiles, any = g.steps > 0;
       const float ta = lg_ref == -INFINITY ? -INFINITY : m + lg_ref;
@@ -637,13 +733,13 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         threads_meet<C::SOFT>();
         if (threadIdx.x == 0) {
           uint32_t seen;
-          asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.counters + c_first) : "memory");
+          asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.counters + c_first * CTAS + rank) : "memory");
           misc[7] = seen == (uint32_t)(parts - 1);
-          if (misc[7]) a.counters[c_first] = 0;
+          if (misc[7]) a.counters[c_first * CTAS + rank] = 0;
         }
         threads_meet<C::SOFT>();
         if (misc[7]) {
-          auto part_of = [&](int c) { return a.parts + ((long long)(c_first + c) * 2 + (c == 0)) * C::PART_FLOATS; };
+          auto part_of = [&](int c) { return a.parts + (((long long)(c_first + c) * CTAS + rank) * 2 + (c == 0)) * C::PART_FLOATS; };
           float top_a = -INFINITY, top_m = -INFINITY, sum_l = 0.0f;
 #pragma unroll 1
           for (int c = 0; c < parts; ++c) {
@@ -682,29 +778,41 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == C::W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (PAIR) {                                                          // the other CTA's MMAs may still read this one's operands, its threads arrive at this one's barriers
+    __syncwarp();
+    cluster_meet();
+    tc_fence_after();
+  }
+  if (warp == C::W_MMA) {
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
 }
 
-template <int D>
+template <int D, int CTAS>
 int launch_as(AttnArgs& a, cudaStream_t st) {
-  using C = ManyCfg<D>;
+  using C = ManyCfg<D, CTAS>;
   static_assert(C::SMEM_BYTES <= 232448, "shared memory of a CTA");
-  a.Gc = a.G < C::R ? a.G : C::R;
+  constexpr int ROWS = C::R * CTAS;
+  a.Gc = a.G < ROWS ? a.G : ROWS;
   a.chunks = (a.G + a.Gc - 1) / a.Gc;
-  a.tq = C::R / a.Gc;
+  a.tq = ROWS / a.Gc;
   CUtensorMap map_k, map_v;
-  RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, a.c.page));
-  RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page));
+  RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, CTAS == 2 && a.c.page > 32 ? 32 : a.c.page, D));
+  RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page, C::V_DIMS));
   static std::atomic<uint64_t> allowed{0};
-  RAZER_TRY(allow_smem((const void*)attn_kv8_many_kernel<D>, C::SMEM_BYTES, allowed));
-  return launch_dependent("attn_kv8_many_kernel launch", attn_kv8_many_kernel<D>, sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS, C::THREADS, C::SMEM_BYTES, st, map_k,
-                          map_v, a);
+  RAZER_TRY(allow_smem((const void*)attn_kv8_many_kernel<D, CTAS>, C::SMEM_BYTES, allowed));
+  const int ctas = (sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS) / CTAS * CTAS;
+  return launch_dependent_clusters("attn_kv8_many_kernel launch", attn_kv8_many_kernel<D, CTAS>, dim3((unsigned)ctas), CTAS, C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
 }
 
 }  // namespace
 
-size_t attn_many_part_floats(int D) { return D == 64 ? ManyCfg<64>::PART_FLOATS : ManyCfg<128>::PART_FLOATS; }
+size_t attn_many_part_floats(int D) { return D == 64 ? ManyCfg<64, 1>::PART_FLOATS : ManyCfg<128, 1>::PART_FLOATS; }
 
-int launch_attn_many(AttnArgs& a, cudaStream_t st) { return a.c.D == 64 ? launch_as<64>(a, st) : launch_as<128>(a, st); }
+int launch_attn_many(AttnArgs& a, bool pairs, cudaStream_t st) {
+  if (a.c.D == 64) return launch_as<64, 1>(a, st);
+  return pairs ? launch_as<128, 2>(a, st) : launch_as<128, 1>(a, st);
+}
 
 }  // namespace razer

@@ -40,14 +40,6 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
       "r"(a_lo), "r"(b_lo), "r"(I8_DESC_HI), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_meet() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ int4 peer_lds128(uint32_t addr, uint32_t rank) {
   int4 v;
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [a];\n\t}"
@@ -295,18 +287,6 @@ __device__ __forceinline__ void mma_i8_pair(uint32_t d_tmem, uint32_t a_lo, uint
       "tcgen05.mma.cta_group::2.kind::i8 [%0], ad, bd, %4, p;\n\t}" ::"r"(d_tmem),
       "r"(a_lo), "r"(b_lo), "r"(I8_DESC_HI), "r"(idesc), "r"(accumulate)
       : "memory");
-}
-// Arrives at the barrier of this offset in every CTA of `mask` once the MMAs issued so far are complete.
-__device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t mask) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)mask) : "memory");
-}
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void peer_arrive(uint32_t addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 // A box into this CTA's shared memory whose bytes are counted by a barrier of the pair's first CTA.
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {

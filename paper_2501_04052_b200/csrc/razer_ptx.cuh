@@ -26,15 +26,25 @@ __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
 // completes (or about the hinted time passes) instead of spinning in the issue slots that
 // the decoding warps need.
 constexpr uint32_t WAIT_SLICE_NS = 1000000u;
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(WAIT_SLICE_NS)
-      : "memory");
+  if (CLUSTER)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(WAIT_SLICE_NS)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(WAIT_SLICE_NS)
+        : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ uint64_t global_ns() {
@@ -48,11 +58,13 @@ __device__ __forceinline__ uint64_t global_ns() {
 constexpr uint32_t WAIT_POLLS = 256;
 constexpr uint64_t WAIT_REST_NS = WAIT_LIMIT_NS - 2ull * WAIT_POLLS * WAIT_SLICE_NS;
 static_assert(2ull * WAIT_POLLS * WAIT_SLICE_NS < WAIT_LIMIT_NS, "the looks before and after the count are part of the limit");
+// CLUSTER: for what threads of another CTA of the cluster wrote before they arrived.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
+  if (mbar_try_wait<CLUSTER>(bar, parity)) return true;
   uint64_t t0 = 0;
   for (uint32_t i = 1;; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_try_wait<CLUSTER>(bar, parity)) return true;
     if (*abort_flag) return false;
     if (i % WAIT_POLLS == 0) {
       const uint64_t t = global_ns();

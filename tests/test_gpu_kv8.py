@@ -410,9 +410,9 @@ def test_a_decode_step_as_it_is_used(b):
     check_attn(b, s, q)
 
 
-@pytest.mark.parametrize("kernel", ["few", "many"])
+@pytest.mark.parametrize("kernel", ["few", "many", "pair"])
 def test_attn_either_kernel_takes_any_batch(kernel):
-    """The attention's tests with all calls on one of its two kernels (the choice is read once a process)."""
+    """The attention's tests with all calls on one of its kernels (the choice is read once a process)."""
     here = os.path.abspath(__file__)
     r = subprocess.run([sys.executable, "-m", "pytest", here, "-q", "-x", "-m", "gpu", "-k", "attn and not either_kernel and not beyond_32_bits"],
                        env=dict(os.environ, RAZER_ATTN=kernel), capture_output=True, text=True, timeout=600)
