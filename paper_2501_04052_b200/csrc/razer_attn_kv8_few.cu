@@ -46,7 +46,7 @@ struct FewCfg {
   static constexpr int O_JOIN = JOIN_ON_P ? O_P : O_P + GROUPS * P_BYTES;
   static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][2][4 warps][R]
   static constexpr int O_STAT = O_RED + GROUPS * 8 * R * 4;            // [group][R] A, M; [group][4][R] sums
-  static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][TABLES][R][8] what a tile means for each row
+  static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][TABLES][8][R] what a tile means for each row
   static constexpr int O_ROW = O_TABLE + 4 * GROUPS * TABLES * R * 32; // [2][R] score factor in two parts; [2][R] keys
   static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] {key scale, log2 of the value scale}, [STAGES] the largest of the latter
   static constexpr int O_BAR = (O_META + STAGES * 68 + 7) / 8 * 8;
@@ -72,6 +72,23 @@ __device__ __forceinline__ float reduce8(const float (&v)[8], int lane, Op op) {
   return op(c, __shfl_xor_sync(0xFFFFFFFFu, c, 1));
 }
 __device__ __forceinline__ int reduce8_row(int lane) { return ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1); }
+
+// The largest over a warp (NaN counts as none), in all lanes.
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
+  return r;
+}
+// Eight numbers of shared memory as four pairs.
+__device__ __forceinline__ void pairs8(const float* p, uint64_t (&v)[4]) {
+  const ulonglong2 a = reinterpret_cast<const ulonglong2*>(p)[0], b = reinterpret_cast<const ulonglong2*>(p)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+// 65536 d2 + 256 d1 + d0 of the rows 2 j and 2 j + 1 of eight: columns d0 of all rows, d1, d2.
+__device__ __forceinline__ uint64_t join_digits(const uint32_t (&x)[24], int j) {
+  const uint64_t low = pair64((float)((int)x[8 + 2 * j] * 256 + (int)x[2 * j]), (float)((int)x[9 + 2 * j] * 256 + (int)x[2 * j + 1]));
+  return fma2(pair64((float)(int)x[16 + 2 * j], (float)(int)x[17 + 2 * j]), pair64(65536.0f, 65536.0f), low);
+}
 
 __device__ __forceinline__ void mma_digits(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -107,8 +124,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
   uint32_t* broken = reinterpret_cast<uint32_t*>(misc + 8);              // [group] rows that saw a value scale that is none
   float2* meta = reinterpret_cast<float2*>(sm + C::O_META);
   float* meta_top = reinterpret_cast<float*>(meta + 8 * ST);
-  float2* row_scale = reinterpret_cast<float2*>(sm + C::O_ROW);           // [2][R]
-  int* row_keys = reinterpret_cast<int*>(row_scale + 2 * R);              // [2][R]
+  float* row_scale = reinterpret_cast<float*>(sm + C::O_ROW);             // [2][2][R] the score factor in two parts
+  int* row_keys = reinterpret_cast<int*>(row_scale + 4 * R);              // [2][R]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -264,8 +281,9 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         const int e = top > 0 && !bad ? ilogbf(__uint_as_float(top)) : 0;
         const float up0 = power2((21 - e) / 2), up1 = power2(21 - e - (21 - e) / 2);
         if (part == 0) {
-          row_scale[buf * R + r] = make_float2(bad ? __uint_as_float(0x7FC00000u) : a.scale * LOG2E * power2(e / 2), power2(e - e / 2 - 21));
-          row_keys[buf * R + r] = real ? max(at.len - at.n + i + 1, 0) : 0;
+          row_scale[2 * buf * R + r] = bad ? __uint_as_float(0x7FC00000u) : a.scale * LOG2E * power2(e / 2);
+          row_scale[(2 * buf + 1) * R + r] = power2(e - e / 2 - 21);
+          row_keys[buf * R + r] = real ? max(at.len - at.n + i + 1, 0) : 0x7FFFFFFF;
         }
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -393,9 +411,10 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     for (int n = 0;; ++n) {
       const Seg s = segment(at);
       const int buf = n & 1, n_tiles = s.last - s.first;
-      float o[R], l[R], top_a = -INFINITY, top_m = -INFINITY;                          // lane r: what row r's sums are relative to
+      uint64_t o[R / 2], l[R / 2];                                                     // of pairs of rows
+      float top_a = -INFINITY, top_m = -INFINITY;                          // lane r: what row r's sums are relative to
 #pragma unroll
-      for (int r = 0; r < R; ++r) o[r] = l[r] = 0.0f;
+      for (int r = 0; r < R / 2; ++r) o[r] = l[r] = 0;
       if (!mbar_wait(bar_qfull + 8 * buf, (uint32_t)((n >> 1) & 1), abort_flag)) fail(7);
       __syncwarp();
       int see_all = 0x7FFFFFFF;                                                       // keys that every row sees
@@ -404,11 +423,11 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       // O of the group's last tile into the running sums; the registers come first, so that the next product may begin
       uint32_t x_o[CHUNKS == 1 ? 24 : 1];
       auto take = [&](int c, const uint32_t (&x)[24], const float* t) {
-        float2 f[8];
+        uint64_t so_far[4], now[4];
+        pairs8(t + 3 * R + 8 * c, so_far);
+        pairs8(t + 4 * R + 8 * c, now);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float2*>(t + (8 * c + j) * 8 + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[8 * c + j] = o[8 * c + j] * f[j].x + f[j].y * __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
+        for (int j = 0; j < 4; ++j) o[4 * c + j] = fma2(o[4 * c + j], so_far[j], mul2(now[j], join_digits(x, j)));
       };
       auto load24 = [&](uint32_t t, uint32_t (&x)[24]) {
         tc_ld8(t, x);
@@ -441,30 +460,38 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         if (!mbar_wait(bar_sfull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(8);
         __syncwarp();
         tc_fence_after();
-        float v[R];
-        uint32_t seen = 0;
+        uint64_t v[R / 2];
+        uint32_t seen = 0xFFFFFFFFu;                                                  // rows that see the token
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          float2 f[8];
-          int keys[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            f[j] = row_scale[buf * R + 8 * c + j];
-            keys[j] = edge ? row_keys[buf * R + 8 * c + j] : 0x7FFFFFFF;
-          }
+          uint64_t f0[4], f1[4], w[4];
+          pairs8(row_scale + 2 * buf * R + 8 * c, f0);
+          pairs8(row_scale + (2 * buf + 1) * R + 8 * c, f1);
           uint32_t x[24];
           load24(t_s + 24 * c, x);
-          float w[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = 8 * c + j;
-            const float dot = __fmaf_rn((float)(int)x[16 + j], 65536.0f, (float)((int)x[8 + j] * 256 + (int)x[j]));
-            v[r] = tok < keys[j] ? dot * (sc.x * f[j].x) * f[j].y : -INFINITY;
-            seen |= tok < keys[j] ? 1u << r : 0u;
-            w[j] = v[r] + lg_max;
+          for (int j = 0; j < 4; ++j) v[4 * c + j] = mul2(mul2(join_digits(x, j), mul2(pair64(sc.x, sc.x), f0[j])), f1[j]);
+          if (edge) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const bool s0 = tok < row_keys[buf * R + 8 * c + 2 * j], s1 = tok < row_keys[buf * R + 8 * c + 2 * j + 1];
+              v[4 * c + j] = pair64(s0 ? low64(v[4 * c + j]) : -INFINITY, s1 ? high64(v[4 * c + j]) : -INFINITY);
+              if (!s0) seen &= ~(1u << (8 * c + 2 * j));
+              if (!s1) seen &= ~(2u << (8 * c + 2 * j));
+            }
           }
-          const float t = reduce8(w, lane, [](float x, float y) { return fmaxf(x, y); });
-          if ((lane & 3) == 0) red_now[quarter * R + 8 * c + reduce8_row(lane)] = t;
+          float t[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = add2(v[4 * c + j], pair64(lg_max, lg_max));
+            t[2 * j] = warp_max(low64(w[j]));
+            t[2 * j + 1] = warp_max(high64(w[j]));
+          }
+          if (lane == 0) {
+            float4* to = reinterpret_cast<float4*>(red_now + quarter * R + 8 * c);
+            to[0] = make_float4(t[0], t[1], t[2], t[3]);
+            to[1] = make_float4(t[4], t[5], t[6], t[7]);
+          }
         }
         if (lg != lg && seen) atomicOr(broken + group, seen);                         // a value scale that is none
         // The last tile's product has read its digits by then, and gives way to this one's once it is in registers: late for eight rows, here for more.
@@ -476,24 +503,29 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           for (int q = 0; q < 4; ++q) top = fmaxf(top, red_now[q * R + lane]);
           const float mn = fmaxf(top_m, top - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
           const float an = fmaxf(top_a, top), as = an == -INFINITY ? 0.0f : an;
-          float4* to = reinterpret_cast<float4*>(tab + lane * 8);
-          to[0] = make_float4(ms, top == -INFINITY ? 0.0f : top, ex2(top_m - ms), 0.0f);
-          to[1] = make_float4(ex2(top_a - as), (top == -INFINITY ? 0.0f : ex2(top - as)), 0.0f, 0.0f);   // O so far, the tile's O
+          tab[lane] = -ms;
+          tab[R + lane] = top == -INFINITY ? 0.0f : -top;
+          tab[2 * R + lane] = ex2(top_m - ms);
+          tab[3 * R + lane] = ex2(top_a - as);                                        // O so far
+          tab[4 * R + lane] = top == -INFINITY ? 0.0f : ex2(top - as);                // the tile's O
           top_m = mn, top_a = an;
         }
         __syncwarp();
         const float lg_w = lg != lg ? -INFINITY : lg;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          float4 f[8];
+          uint64_t ms[4], top[4], so_far[4];
           uint32_t u[8];
+          pairs8(tab + 8 * c, ms);
+          pairs8(tab + R + 8 * c, top);
+          pairs8(tab + 2 * R + 8 * c, so_far);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float4*>(tab + (8 * c + j) * 8);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = 8 * c + j;
-            l[r] = __fmaf_rn(l[r], f[j].z, ex2(v[r] - f[j].x));
-            u[j] = __float2uint_rn(ex2(v[r] + lg_w - f[j].y) * W_ONE);
+          for (int j = 0; j < 4; ++j) {
+            const uint64_t p = v[4 * c + j], e = add2(p, ms[j]), w = add2(add2(p, pair64(lg_w, lg_w)), top[j]);
+            l[4 * c + j] = fma2(l[4 * c + j], so_far[j], pair64(ex2(low64(e)), ex2(high64(e))));
+            const uint64_t b = mul2(pair64(ex2(low64(w)), ex2(high64(w))), pair64(W_ONE, W_ONE));
+            u[2 * j] = __float2uint_rn(low64(b));
+            u[2 * j + 1] = __float2uint_rn(high64(b));
           }
           if (CHUNKS == 1 && pending) {
             if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)((mine - 1) & 1), abort_flag)) fail(10);
@@ -524,7 +556,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       for (int c = 0; c < CHUNKS; ++c) {
         float w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = l[8 * c + j];
+        for (int j = 0; j < 8; ++j) w[j] = (j & 1) ? high64(l[4 * c + j / 2]) : low64(l[4 * c + j / 2]);
         const float t = reduce8(w, lane, [](float x, float y) { return x + y; });
         if ((lane & 3) == 0) stat_l[quarter * R + 8 * c + reduce8_row(lane)] = t;
       }
@@ -538,7 +570,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       for (int c = 0; c < CHUNKS; ++c) {
         if (has_dim) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) join[(group * 8 + j) * D + dim] = o[8 * c + j];
+          for (int j = 0; j < 8; ++j) join[(group * 8 + j) * D + dim] = (j & 1) ? high64(o[4 * c + j / 2]) : low64(o[4 * c + j / 2]);
         }
         threads_meet<SOFT>();
         for (int x = threadIdx.x; x < 8 * (D / 4); x += SOFT) {
