@@ -10,14 +10,15 @@
 // width up to 64), they cost nothing, and a tile takes a third of the instructions that unpacking codes for mma.sync took.
 //
 // Roles: a warp each brings keys and values (pages and scales looked up 32 at a time), one prepares the queries of the next unit, one issues
-// MMAs, and GROUPS groups of four warps take the tiles in turn: maximum over the tile (nine shuffles for eight rows, then the four warps
+// MMAs, and GROUPS groups of four warps take the tiles in turn: maximum over the tile (a warp reduction a row, then the four warps
 // through shared memory), exponentials, digits to shared memory, and O = O f + O_tile in FP32 registers.  Work is cut evenly
 // among the CTAs as razer_attn_kv8.cuh says.
 //
-// What bounds it: 64 sequences of up to 16384 tokens, 8 x 8 heads of 128 (1.28 GB) 206 us, 6.2 TB/s, as long as the clock is up; in a loop of
-// some seconds the GPU is at its power limit (1000 W, 1675 instead of 1965 MHz) and the call takes 240.  One sequence of 4096 tokens, 8 x 4 heads of 64:
-// 12.0, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  With heads of 64 and pages of 16, the cost of a tile
-// (1400 cycles for 128 tokens, 16 KB).
+// What bounds it: instructions, then HBM.  64 sequences of up to 16384 tokens, 8 x 8 heads of 128 (1.28 GB) 201 to 214 us (6.0 to 6.4 TB/s) as long as the clock is up; in
+// a loop of some seconds the GPU is at its power limit (1000 W, 1700 instead of 1965 MHz) and the call takes 228 (241 before rows went two to an instruction, packed
+// FP32, and maxima by redux.sync).  32 sequences of 4096 tokens: 54 us for 8 rows, 76 for 16, 121 for 32 (83 and 169 before that).  One sequence of 4096 tokens, 8 x 4 heads
+// of 64: 11.6, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  Heads of 64: 79 us for 268 MB in pages of 64, 95 in pages
+// of 16 (boxes of 1 KB).
 #include "razer_attn_kv8.cuh"
 
 namespace razer {
@@ -58,20 +59,19 @@ struct FewCfg {
   static constexpr int PART_FLOATS = R * (D + 3);                      // a part of a unit: O, A, M, sum
 };
 
-// The largest of each of eight values over a warp: nine shuffles; lane gets that of value 4 bit4 + 2 bit3 + bit2 of its number.
-template <class Op>
-__device__ __forceinline__ float reduce8(const float (&v)[8], int lane, Op op) {
+// The sum of each of eight values over a warp: nine shuffles; lane gets that of value sum8_row.
+__device__ __forceinline__ float sum8(const float (&v)[8], int lane) {
   float a[4], b[2];
   const bool h4 = lane & 16, h3 = lane & 8, h2 = lane & 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = op(h4 ? v[4 + i] : v[i], __shfl_xor_sync(0xFFFFFFFFu, h4 ? v[i] : v[4 + i], 16));
+  for (int i = 0; i < 4; ++i) a[i] = (h4 ? v[4 + i] : v[i]) + __shfl_xor_sync(0xFFFFFFFFu, h4 ? v[i] : v[4 + i], 16);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) b[i] = op(h3 ? a[2 + i] : a[i], __shfl_xor_sync(0xFFFFFFFFu, h3 ? a[i] : a[2 + i], 8));
-  float c = op(h2 ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, h2 ? b[0] : b[1], 4));
-  c = op(c, __shfl_xor_sync(0xFFFFFFFFu, c, 2));
-  return op(c, __shfl_xor_sync(0xFFFFFFFFu, c, 1));
+  for (int i = 0; i < 2; ++i) b[i] = (h3 ? a[2 + i] : a[i]) + __shfl_xor_sync(0xFFFFFFFFu, h3 ? a[i] : a[2 + i], 8);
+  float c = (h2 ? b[1] : b[0]) + __shfl_xor_sync(0xFFFFFFFFu, h2 ? b[0] : b[1], 4);
+  c += __shfl_xor_sync(0xFFFFFFFFu, c, 2);
+  return c + __shfl_xor_sync(0xFFFFFFFFu, c, 1);
 }
-__device__ __forceinline__ int reduce8_row(int lane) { return ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1); }
+__device__ __forceinline__ int sum8_row(int lane) { return ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1); }
 
 // The largest over a warp (NaN counts as none), in all lanes.
 __device__ __forceinline__ float warp_max(float v) {
@@ -106,12 +106,16 @@ __device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t* v) {
                : "r"(taddr)
                : "memory");
 }
+__device__ __forceinline__ void tc_ld4(uint32_t taddr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void sts8(uint32_t addr, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 
-template <int D, int R>
+template <int D, int R, int LIVE>
 __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                                 const __grid_constant__ AttnArgs a) {
   using C = FewCfg<D, R>;
+  constexpr int LP = LIVE < 8 ? LIVE / 2 : 4;                              // pairs of rows of eight that are worked on
   constexpr int TK = C::TK, ST = C::STAGES, GROUPS = C::GROUPS, CHUNKS = C::CHUNKS, SOFT = 128 * GROUPS;
   extern __shared__ uint8_t attn_smem[];
   uint8_t* sm = attn_smem + ((1024 - (smem_u32(attn_smem) & 1023)) & 1023);
@@ -427,12 +431,18 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         pairs8(t + 3 * R + 8 * c, so_far);
         pairs8(t + 4 * R + 8 * c, now);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[4 * c + j] = fma2(o[4 * c + j], so_far[j], mul2(now[j], join_digits(x, j)));
+        for (int j = 0; j < LP; ++j) o[4 * c + j] = fma2(o[4 * c + j], so_far[j], mul2(now[j], join_digits(x, j)));
       };
       auto load24 = [&](uint32_t t, uint32_t (&x)[24]) {
-        tc_ld8(t, x);
-        tc_ld8(t + 8, x + 8);
-        tc_ld8(t + 16, x + 16);
+        if (LP == 4) {
+          tc_ld8(t, x);
+          tc_ld8(t + 8, x + 8);
+          tc_ld8(t + 16, x + 16);
+        } else {
+          tc_ld4(t, x);
+          tc_ld4(t + 8, x + 8);
+          tc_ld4(t + 16, x + 16);
+        }
         tc_wait_ld();
       };
       bool pending = false;                                                           // the last tile's product with the values is not in yet
@@ -470,19 +480,19 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           uint32_t x[24];
           load24(t_s + 24 * c, x);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[4 * c + j] = mul2(mul2(join_digits(x, j), mul2(pair64(sc.x, sc.x), f0[j])), f1[j]);
+          for (int j = 0; j < LP; ++j) v[4 * c + j] = mul2(mul2(join_digits(x, j), mul2(pair64(sc.x, sc.x), f0[j])), f1[j]);
           if (edge) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < LP; ++j) {
               const bool s0 = tok < row_keys[buf * R + 8 * c + 2 * j], s1 = tok < row_keys[buf * R + 8 * c + 2 * j + 1];
               v[4 * c + j] = pair64(s0 ? low64(v[4 * c + j]) : -INFINITY, s1 ? high64(v[4 * c + j]) : -INFINITY);
               if (!s0) seen &= ~(1u << (8 * c + 2 * j));
               if (!s1) seen &= ~(2u << (8 * c + 2 * j));
             }
           }
-          float t[8];
+          float t[8] = {};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < LP; ++j) {
             w[j] = add2(v[4 * c + j], pair64(lg_max, lg_max));
             t[2 * j] = warp_max(low64(w[j]));
             t[2 * j + 1] = warp_max(high64(w[j]));
@@ -490,7 +500,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           if (lane == 0) {
             float4* to = reinterpret_cast<float4*>(red_now + quarter * R + 8 * c);
             to[0] = make_float4(t[0], t[1], t[2], t[3]);
-            to[1] = make_float4(t[4], t[5], t[6], t[7]);
+            if (LP == 4) to[1] = make_float4(t[4], t[5], t[6], t[7]);
           }
         }
         if (lg != lg && seen) atomicOr(broken + group, seen);                         // a value scale that is none
@@ -520,7 +530,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           pairs8(tab + R + 8 * c, top);
           pairs8(tab + 2 * R + 8 * c, so_far);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < LP; ++j) {
             const uint64_t p = v[4 * c + j], e = add2(p, ms[j]), w = add2(add2(p, pair64(lg_w, lg_w)), top[j]);
             l[4 * c + j] = fma2(l[4 * c + j], so_far[j], pair64(ex2(low64(e)), ex2(high64(e))));
             const uint64_t b = mul2(pair64(ex2(low64(w)), ex2(high64(w))), pair64(W_ONE, W_ONE));
@@ -534,7 +544,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
             load24(t_o, reinterpret_cast<uint32_t(&)[24]>(x_o));
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < 2 * LP; ++j) {
             const uint32_t to = p_at + (24 * c + j) * TK + (tid ^ (j << 4));
             sts8(to, u[j]);
             sts8(to + 8 * TK, u[j] >> 8);
@@ -557,8 +567,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         float w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = (j & 1) ? high64(l[4 * c + j / 2]) : low64(l[4 * c + j / 2]);
-        const float t = reduce8(w, lane, [](float x, float y) { return x + y; });
-        if ((lane & 3) == 0) stat_l[quarter * R + 8 * c + reduce8_row(lane)] = t;
+        const float t = sum8(w, lane);
+        if ((lane & 3) == 0) stat_l[quarter * R + 8 * c + sum8_row(lane)] = t;
       }
       if (quarter == 0 && lane < R) stat_a[lane] = top_a, stat_m[lane] = top_m;
       threads_meet<SOFT>();
@@ -616,19 +626,20 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
   if (warp == C::W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::TMEM_COLS) : "memory");
 }
 
-template <int D, int R>
+// LIVE: rows of a row tile, R or half of 8: what is computed of a tile's scores and sums goes by it, the columns that the MMAs compute by R.
+template <int D, int R, int LIVE = R>
 int launch_as(AttnArgs& a, cudaStream_t st) {
   using C = FewCfg<D, R>;
   static_assert(C::SMEM_BYTES <= 232448, "shared memory of a CTA");
-  a.Gc = a.G < R ? a.G : R;
+  a.Gc = a.G < LIVE ? a.G : LIVE;
   a.chunks = (a.G + a.Gc - 1) / a.Gc;
-  a.tq = R / a.Gc;
+  a.tq = LIVE / a.Gc;
   CUtensorMap map_k, map_v;
   RAZER_TRY(attn_encode_pool(&map_k, a.c.k, a.c, a.c.page, D));
   RAZER_TRY(attn_encode_pool(&map_v, a.c.v, a.c, a.c.page, D));
   static std::atomic<uint64_t> allowed{0};
-  RAZER_TRY(allow_smem((const void*)attn_kv8_few_kernel<D, R>, C::SMEM_BYTES, allowed));
-  return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R>, sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS, C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
+  RAZER_TRY(allow_smem((const void*)attn_kv8_few_kernel<D, R, LIVE>, C::SMEM_BYTES, allowed));
+  return launch_dependent("attn_kv8_few_kernel launch", attn_kv8_few_kernel<D, R, LIVE>, sm_count() < ATTN_CTAS ? sm_count() : ATTN_CTAS, C::THREADS, C::SMEM_BYTES, st, map_k, map_v, a);
 }
 
 }  // namespace
@@ -636,6 +647,8 @@ int launch_as(AttnArgs& a, cudaStream_t st) {
 size_t attn_few_part_floats(int D) { return D == 64 ? FewCfg<64, 32>::PART_FLOATS : FewCfg<128, 32>::PART_FLOATS; }
 
 int launch_attn_few(AttnArgs& a, int rows, cudaStream_t st) {
+  // Four rows at most (64 sequences of 4096 tokens, 8 x 4 heads): half of eight's work, heads of 64 79 us against 88, of 128 (32 sequences) 55 against 57.
+  if (rows <= 4) return a.c.D == 64 ? launch_as<64, 8, 4>(a, st) : launch_as<128, 8, 4>(a, st);
   if (a.c.D == 64) return rows <= 8 ? launch_as<64, 8>(a, st) : rows <= 16 ? launch_as<64, 16>(a, st) : launch_as<64, 32>(a, st);
   return rows <= 8 ? launch_as<128, 8>(a, st) : rows <= 16 ? launch_as<128, 16>(a, st) : launch_as<128, 32>(a, st);
 }
