@@ -109,7 +109,7 @@ __device__ __forceinline__ bool attn_share(const AttnArgs& a, int tokens, int* w
   const bool once = a.s.B <= THREADS;                    // every sequence has a thread: one look at it is enough
   long long total = 0, mine = 0;
   for (int b = threadIdx.x; b < a.s.B; b += THREADS) total += mine = walk_enter(a, tokens, b, at);
-  long long base = 0;                                    // items of the sequences before this round's
+  long long base = 0;                                    // items of the sequences before those looked at
   if (!once) {
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
     if (lane == 0) sums[warp] = total;
