@@ -9,7 +9,8 @@
 // scores are read once.  O stays in TMEM; it is brought to a new maximum only when that has grown by more than 2^8, so that after a unit's
 // first tiles next to never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16
 // times 2^6 (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to
-// twice the largest met.
+// twice the largest that the row has met.  (Of the pages that it sees: one for all rows of a tile would leave a row whose own pages have values 2^33 times
+// smaller than those behind its mask without any weight.)
 // A pair of CTAs (cta_group::2) takes 512 rows: each converts half of the keys of a step and half of the values' dimensions, so that a tile is
 // converted once for both, and the MMAs read half as much of it from either's shared memory.
 // What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 352 us (751 TFLOP/s) by pairs, 373 without: 2300 to 2500 cycles
@@ -47,8 +48,8 @@ struct ManyCfg {
   static constexpr int STAGES = 2 * CTAS;                                     // of codes: with one, a copy's latency was in every tile (194 us of 458 were that skeleton)
   static constexpr int O_CODES = O_V + 2 * PART_BYTES;                     // keys, values of each stage: [K_ROWS][D], [128 tokens][V_DIMS]
   static constexpr int METAS = 8;                                      // tiles whose scales are held: up to four on their way, three in work
-  static constexpr int O_META = O_CODES + 2 * STAGES * TILE_BYTES;     // [METAS][8] {key scale, log2 of the value scale}, [METAS] the largest of the latter
-  static constexpr int O_BAR = O_META + METAS * 68;
+  static constexpr int O_META = O_CODES + 2 * STAGES * TILE_BYTES;     // [METAS][8] {key scale, log2 of the value scale}, [METAS][2] the largest of the latter in a step
+  static constexpr int O_BAR = O_META + METAS * 72;
   static constexpr int N_BAR = 4 * STAGES + 8 + 2 + 4 + 4 + 4 + 1;
   static constexpr int O_MISC = O_BAR + 8 * N_BAR;
   static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
@@ -248,9 +249,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
         const int from = ((lane & 7) * 16) >> a.c.page_log2;
         float k1 = __shfl_sync(0xFFFFFFFFu, ks, (block0 - have + from) & 31), v1 = __shfl_sync(0xFFFFFFFFu, lg, (block0 - have + from) & 31);
         if (from >= live) k1 = 0.0f, v1 = -INFINITY;             // no token that anyone sees
-        float most = v1;
-        for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-        if (!(most > -INFINITY)) most = -INFINITY;
+        float most = fmaxf(v1, -INFINITY);                       // (NaN counts as none)
+        for (int o = 1; o < 4; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
         const int stage = item % C::STAGES, round = item / C::STAGES;
         if (round > 0) {                                         // the codes before have been read
           if (!mbar_wait(bar_read + 8 * stage, (uint32_t)(round & 1) ^ 1u, abort_flag)) fail(1), alive = false;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           if (!alive) break;
         }
         if (lane < 8) meta[item % C::METAS * 8 + lane] = make_float2(k1, v1);
-        if (lane == 0) meta_top[item % C::METAS] = most;
+        if (lane == 0 || lane == 4) meta_top[item % C::METAS * 2 + (lane >> 2)] = most;
         __syncwarp();
         {
           const uint32_t in = bar_in + 8 * stage;
@@ -524,7 +524,6 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           tc_fence_after();
           // The scales were put down before the tile's codes were asked for, and the scores came behind these.  (The barrier of the f16 keys is not for these
           // threads to wait for: it may be two phases further by now, and a parity does not tell.)
-          const float lg_top = meta_top[tile % C::METAS];
           float c[4], lg[4];                                                           // of the step's four times sixteen columns
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -532,12 +531,17 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
             c[q] = sc.x * f1;
             lg[q] = sc.y;
           }
+          float lg_top = meta_top[tile % C::METAS * 2 + (n & 1)];                      // the largest that the row sees
           // ---- the step's scores, and their maximum: of sixteen before their page's scale, which is not negative
           uint32_t v[2][32];
           tc_ld32(t_s + 64 * b, v[0]);
           tc_ld32(t_s + 64 * b + 32, v[1]);
           tc_wait_ld();
           if (edge) {
+            lg_top = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (tok + 16 * q < see) lg_top = fmaxf(lg_top, lg[q]);
 #pragma unroll
             for (int x = 0; x < 64; ++x) v[x / 32][x % 32] = tok + x < see ? v[x / 32][x % 32] : 0xFF800000u;
           }
