@@ -319,8 +319,8 @@ int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_
  * page, and so do a page that the table does not name and a NaN or an infinity among a row's queries; a sequence longer than the table
  * gets NaN in all its rows.  Keys and values count exactly, sums are FP32.  What is rounded follows the kernel, and that the mean of the
  * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head.  Up to 32 rows: queries to 2^-23 of their row's largest
- * magnitude (24-bit fixed point: bf16 exactly down to 2^-14 of it), weights exp(s_j) v_scale to 2^-25 of the largest among 128
- * consecutive keys.  More: both to f16, queries relative to their row's largest magnitude (bf16 exactly down to 2^-28 of it), weights
+ * magnitude (24-bit fixed point: bf16 exactly down to 2^-14 of it), weights exp(s_j) v_scale to 2^-25 of the largest that the
+ * row sees among 128 consecutive keys.  More: both to f16, queries relative to their row's largest magnitude (bf16 exactly down to 2^-28 of it), weights
  * with 11 significant bits or to 2^-30 of the row's largest exp(s_j) times the largest value scale among the pages that it sees.
  * The workspace is that of razer_attn_kv8_workspace_bytes, prepared once by razer_workspace_init; calls that may overlap on the
  * GPU must not share one (two replayed graphs included).  razer_workspace_status reports a wait that gave up. */

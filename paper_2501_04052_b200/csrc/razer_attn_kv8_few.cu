@@ -5,7 +5,9 @@
 //   S[token][row, digit] = K Q^T    q = 2^(e - 21) (65536 d2 + 256 d1 + d0), signed digits, e from the row's largest magnitude
 //   O[dim][row, digit]   = V^T P    w = exp2(s + log2 vs - top) <= 1 held as 24 bits, three unsigned digits, top the tile's own maximum
 // The sums are exact in 32 bits, so that what is rounded is q to 2^-23 of its row's largest (bf16 queries exactly but for those below 2^-14
-// of it), w to 2^-25 of the tile's largest, and the FP32 arithmetic between.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each
+// of it), w to 2^-25 of the tile's largest, and the FP32 arithmetic between.  One maximum serves both sums, of s + max(log2 vs, the tile's largest - 60): it
+// stays above every weight, and within 2^60 of the largest exponential.  Where value scales of a tile lie further apart (a page of zeros too) it may be far above the
+// weights that there are; their own is then found in a second round.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each
 // dimension for O.  Since the digits ride along as columns (32 of S and of O for 8 rows, against 54 cycles that an MMA takes at any
 // width up to 64), they cost nothing, and a tile takes a third of the instructions that unpacking codes for mma.sync took.
 //
@@ -26,6 +28,7 @@ namespace razer {
 namespace {
 
 constexpr float W_ONE = 16777215.0f;                                   // what a weight of 1 is held as: 24 bits
+constexpr float FLOOR = 60.0f;                                         // how far (log2) below the tile's largest value scale a token's counts as in the common maximum
 
 template <int D_, int R_>
 struct FewCfg {
@@ -49,8 +52,8 @@ struct FewCfg {
   static constexpr int O_STAT = O_RED + GROUPS * 8 * R * 4;            // [group][R] A, M; [group][4][R] sums
   static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][TABLES][8][R] what a tile means for each row
   static constexpr int O_ROW = O_TABLE + 4 * GROUPS * TABLES * R * 32; // [2][R] score factor in two parts; [2][R] keys
-  static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] {key scale, log2 of the value scale}, [STAGES] the largest of the latter
-  static constexpr int O_BAR = (O_META + STAGES * 68 + 7) / 8 * 8;
+  static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] {key scale, log2 of the value scale}, [STAGES] {the largest of the latter, whether they lie far apart}
+  static constexpr int O_BAR = (O_META + STAGES * 72 + 7) / 8 * 8;
   static constexpr int N_BAR = 3 * STAGES + 3 * GROUPS + 5;
   static constexpr int O_MISC = O_BAR + 8 * N_BAR;                     // words: abort, never set, share (4 words), TMEM, last, broken values by group, sums
   static constexpr int SMEM_BYTES = 1024 + O_MISC + 256;
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
   volatile uint32_t* never = reinterpret_cast<uint32_t*>(misc + 1);
   uint32_t* broken = reinterpret_cast<uint32_t*>(misc + 8);              // [group] rows that saw a value scale that is none
   float2* meta = reinterpret_cast<float2*>(sm + C::O_META);
-  float* meta_top = reinterpret_cast<float*>(meta + 8 * ST);
+  float2* meta_top = meta + 8 * ST;
   float* row_scale = reinterpret_cast<float*>(sm + C::O_ROW);             // [2][2][R] the score factor in two parts
   int* row_keys = reinterpret_cast<int*>(row_scale + 4 * R);              // [2][R]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -243,9 +246,10 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
           if (lane >= live) k1 = 0.0f, v1 = -INFINITY;           // no token that anyone sees
           float most = v1;
           for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+          const bool apart = __any_sync(0xFFFFFFFFu, lane < live && v1 < most - FLOOR);      // (live: up to 8; false where all are 0)
           if (!(most > -INFINITY)) most = 0.0f;                  // all of them 0 or broken
           if (lane < 8) meta[stage * 8 + lane] = make_float2(k1, v1);
-          if (lane == 0) meta_top[stage] = most;
+          if (lane == 0) meta_top[stage] = make_float2(most, apart ? 1.0f : 0.0f);
           __syncwarp();
         }
         if (lane == 0) mbar_expect_tx(bar, (uint32_t)((live << a.c.page_log2) * D));
@@ -445,6 +449,12 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         }
         tc_wait_ld();
       };
+      auto row_top = [&](const float* red_now) {                                      // of row `lane`, from the four warps
+        float top = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) top = fmaxf(top, red_now[q * R + lane]);
+        return top;
+      };
       bool pending = false;                                                           // the last tile's product with the values is not in yet
       auto take_all = [&]() {
         if (!mbar_wait(bar_ofull + 8 * group, (uint32_t)((mine - 1) & 1), abort_flag)) fail(10);
@@ -466,7 +476,9 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         // the values' barrier first: their warp has the scales
         if (!mbar_wait(bar_vfull + 8 * stage, (uint32_t)(((item + i) / ST) & 1), abort_flag)) fail(9);
         const float2 sc = meta[stage * 8 + (tid >> a.c.page_log2)];
-        const float lg_top = meta_top[stage], lg = sc.y, lg_max = fmaxf(lg, lg_top - 60.0f);   // (a NaN becomes the floor)
+        const float2 most = meta_top[stage];
+        const bool apart = most.y != 0.0f;
+        const float lg_top = most.x, lg = sc.y, lg_max = fmaxf(lg, lg_top - FLOOR);   // (a NaN becomes the floor)
         if (!mbar_wait(bar_sfull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(8);
         __syncwarp();
         tc_fence_after();
@@ -507,11 +519,24 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         // The last tile's product has read its digits by then, and gives way to this one's once it is in registers: late for eight rows, here for more.
         if (CHUNKS > 1 && pending) take_all();
         group_meet(group);
-        if (lane < R) {                                                               // what all threads want to know of row `lane`
-          float top = -INFINITY;
+        float common = 0.0f;                                                          // the maximum with the floor
+        if (apart) {
+          // Some value scale here is so much smaller than the largest that the floor may have made the maximum, above all weights that there are: once more without it.
+          common = lane < R ? row_top(red_now) : 0.0f;
+          group_meet(group);
+          const uint64_t own = pair64(lg != lg ? -INFINITY : lg, lg != lg ? -INFINITY : lg);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) top = fmaxf(top, red_now[q * R + lane]);
-          const float mn = fmaxf(top_m, top - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
+          for (int j = 0; j < R / 8 * LP; ++j) {
+            const int r = j / LP * 8 + j % LP * 2;
+            const uint64_t w = add2(v[r / 2], own);
+            const float t0 = warp_max(low64(w)), t1 = warp_max(high64(w));
+            if (lane == 0) red_now[quarter * R + r] = t0, red_now[quarter * R + r + 1] = t1;
+          }
+          group_meet(group);
+        }
+        if (lane < R) {                                                               // what all threads want to know of row `lane`
+          const float top = row_top(red_now);
+          const float mn = fmaxf(top_m, (apart ? common : top) - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
           const float an = fmaxf(top_a, top), as = an == -INFINITY ? 0.0f : an;
           tab[lane] = -ms;
           tab[R + lane] = top == -INFINITY ? 0.0f : -top;

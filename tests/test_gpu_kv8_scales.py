@@ -52,8 +52,8 @@ def check_rows(b, s, q, few):  # noqa: F811
     return got, got_lse
 
 
-# new tokens, query heads a group, dimensions: 60, 300 rows; 1024 rows and more (pairs of CTAs)
-SHAPES = [(60, 1, 64), (75, 4, 128), (260, 4, 128)]
+# new tokens, query heads a group, dimensions: 4, 8, 16, 32 rows; 60, 300 rows; 1024 rows and more (pairs of CTAs)
+SHAPES = [(4, 1, 64), (8, 1, 128), (4, 4, 128), (32, 1, 64), (16, 2, 128), (60, 1, 64), (75, 4, 128), (260, 4, 128)]
 
 
 @pytest.mark.parametrize("power", [20, 40, 75])
@@ -67,7 +67,8 @@ def test_value_scales_of_hidden_pages(b, n, G, D, power):  # noqa: F811
 
 @pytest.mark.parametrize("n,G,D", SHAPES)
 def test_values_behind_the_mask_change_nothing(b, n, G, D):  # noqa: F811
-    """Large, small, zero: rows that do not see the page are the same number for number."""
+    """Large, small, zero: rows that do not see the page are the same number for number in the kernel for many rows (in that for few the sum of the exponentials is
+    relative to what the page's tile has, a rounding's difference)."""
     want = None
     for power in (0, 1, 12, 30, -40):
         s = Batch([n], [n + 30], 2, D, 16, seed=n)
@@ -80,3 +81,32 @@ def test_values_behind_the_mask_change_nothing(b, n, G, D):  # noqa: F811
         assert before > 0
         if n * G > 32:
             assert torch.equal(got[:before], want[0]) and torch.equal(lse[:before], want[1]), power
+
+
+@pytest.mark.parametrize("rows", [1, 4, 8, 16, 32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("low", [0.0, 2.0 ** -90, 2.0 ** -61, 2.0 ** -59])
+def test_pages_that_matter_without_the_largest_scores(b, rows, D, low):  # noqa: F811
+    """A page with far larger scores and hardly any values: what comes out is the other pages', to 24 bits of the largest weight among 128 tokens."""
+    s = Batch([1], [300], 1, D, 16, seed=rows)
+    q = torch.full((1, rows, D), 1.0).bfloat16()
+    q += (torch.randint(-4, 5, q.shape, generator=s.g) / 128).bfloat16()
+    for block in (2, 9, 17):                                   # of two tiles of 128 tokens and of the last, which has no full one
+        at = int(s.table[0, block])
+        s.k[at] = 127
+        s.ks[at] = 70.0 / (127 * D ** 0.5)                     # scores of about 70, the others within some units of 0
+        s.vs[at] *= low
+    s.ks[s.table[0, [0, 1]].long()] *= 0.1
+    check_rows(b, s, q, few=True)
+
+
+def test_a_tile_of_values_that_are_all_zero(b):  # noqa: F811
+    """No value scale in 128 tokens, and one in the next; broken ones beside zeros show."""
+    for rows in (1, 8, 32, 40):
+        s = Batch([1], [300], 1, 64, 16, seed=rows)
+        s.vs[s.table[0, :8].long()] = 0.0
+        q = queries(s, rows)
+        check_rows(b, s, q, few=rows <= 32)
+        s.vs[int(s.table[0, 3])] = float("nan")
+        s.device(b)
+        assert torch.isnan(b.razer_attn_kv8(s.cache, q.cuda(), *s.args)[0]).all()
