@@ -318,7 +318,7 @@ int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_
  * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN or negative shows as NaN in the rows that see its
  * page, and so do a page that the table does not name and a NaN or an infinity among a row's queries; a sequence longer than the table
  * gets NaN in all its rows.  Keys and values count exactly, sums are FP32.  What is rounded follows the kernel, and that the mean of the
- * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head.  Up to 32 rows: queries to 2^-23 of their row's largest
+ * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head.  Up to 32 rows: queries to 2^-22 of their row's largest
  * magnitude (24-bit fixed point: bf16 exactly down to 2^-14 of it), weights exp(s_j) v_scale to 2^-25 of the largest that the
  * row sees among 128 consecutive keys.  More: both to f16, queries relative to their row's largest magnitude (bf16 exactly down to 2^-28 of it), weights
  * with 11 significant bits or to 2^-30 of the row's largest exp(s_j) times the largest value scale among the pages that it sees.

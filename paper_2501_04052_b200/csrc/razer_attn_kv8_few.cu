@@ -4,7 +4,7 @@
 // never converted.  Queries and probabilities are operand B, split into 8-bit digits that are columns of their own:
 //   S[token][row, digit] = K Q^T    q = 2^(e - 21) (65536 d2 + 256 d1 + d0), signed digits, e from the row's largest magnitude
 //   O[dim][row, digit]   = V^T P    w = exp2(s + log2 vs - top) <= 1 held as 24 bits, three unsigned digits, top the tile's own maximum
-// The sums are exact in 32 bits, so that what is rounded is q to 2^-23 of its row's largest (bf16 queries exactly but for those below 2^-14
+// The sums are exact in 32 bits, so that what is rounded is q to 2^-22 of its row's largest (bf16 queries exactly but for those below 2^-14
 // of it), w to 2^-25 of the tile's largest, and the FP32 arithmetic between.  One maximum serves both sums, of s + max(log2 vs, the tile's largest - 60): it
 // stays above every weight, and within 2^60 of the largest exponential.  Where value scales of a tile lie further apart (a page of zeros too) it may be far above the
 // weights that there are; their own is then found in a second round.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each

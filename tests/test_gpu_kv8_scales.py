@@ -110,3 +110,24 @@ def test_a_tile_of_values_that_are_all_zero(b):  # noqa: F811
         s.vs[int(s.table[0, 3])] = float("nan")
         s.device(b)
         assert torch.isnan(b.razer_attn_kv8(s.cache, q.cuda(), *s.args)[0]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 8, 32])
+def test_queries_in_24_bit_fixed_point(b, rows):  # noqa: F811
+    """Up to 32 rows: each number of a query is held to 2^-22 of the row's largest (half a step of 2^(e - 21), the largest in [2^e, 2^(e + 1))).  The largest meets no key here,
+    so that a small one is all that the score, which is the log-sum of one key, has."""
+    unit = 64 ** -0.5 * 2.0 ** 13 * 127
+    for first in range(1, 200, rows):
+        s = Batch([1], [1], 1, 64, 16, seed=first)
+        at = int(s.table[0, 0])
+        s.k[at], s.ks[at] = 127, 2.0 ** 13
+        s.k[at, 0, :, 0] = 0
+        q = torch.zeros((1, rows, 64), dtype=torch.float64)
+        q[..., 0] = 1.0
+        for r in range(rows):
+            q[0, r, 1 + r % 63] = (first + r) * 2.0 ** -23 * (-1) ** r
+        s.device(b)
+        _, lse = b.razer_attn_kv8(s.cache, q.bfloat16().cuda(), *s.args)
+        want = unit * q[0, :, 1:].sum(1)
+        off = (lse[0].double().cpu() - want).abs()
+        assert (off <= unit * 2.0 ** -22 + (2.0 ** -23 * 68 + 2.0 ** -22) * want.abs() + 2.0 ** -21).all(), (first, float(off.max() / unit))
