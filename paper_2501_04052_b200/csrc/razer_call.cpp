@@ -122,6 +122,16 @@ bool counts(const at::Tensor& t) {
     if (n > INT32_MAX) return false;
   return true;
 }
+// The library's function without the interpreter's lock: a launch may wait for room in its queue, and the device for a Python callback.  Arguments
+// are read before.
+template <class Fn, class... A>
+int unlocked(Fn fn, A... a) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(a...);
+  Py_END_ALLOW_THREADS
+  return rc;
+}
 // The caller's tensor, or a new one where `o` is None; false where it is neither.
 bool given(PyObject* o, at::Tensor& t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
   if (o == Py_None) {
@@ -155,7 +165,7 @@ PyObject* quant_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!given(a[2], codes, x, at::kChar, {M, K}) || !given(a[3], scales, x, at::kFloat, {M}) || !whole(codes, at::kChar, st.device_index(), {M, K}) ||
         !whole(scales, at::kFloat, st.device_index(), {M}))
       Py_RETURN_NONE;
-    const int rc = fn(x.data_ptr(), fp32, (int)M, (int)K, M == 1 ? K : x.stride(0), static_cast<int8_t*>(codes.data_ptr()), static_cast<float*>(scales.data_ptr()), st.stream());
+    const int rc = unlocked(fn, x.data_ptr(), (int)fp32, (int)M, (int)K, M == 1 ? K : x.stride(0), static_cast<int8_t*>(codes.data_ptr()), static_cast<float*>(scales.data_ptr()), st.stream());
     return rc == 0 ? pair_of(codes, scales) : PyLong_FromLong(rc);
   } catch (const std::exception&) {
     Py_RETURN_NONE;
@@ -177,8 +187,8 @@ PyObject* gemm_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!whole(x, at::kChar, dev, {M, K}) || !whole(w, at::kChar, dev, {N, K}) || !whole(sx, at::kFloat, dev, {M}) || !whole(sw, at::kFloat, dev, {N}) ||
         !given(a[5], y, x, at::kBFloat16, {M, N}) || !whole(y, at::kBFloat16, dev, {M, N}))
       Py_RETURN_NONE;
-    const int rc = fn(static_cast<const int8_t*>(x.data_ptr()), static_cast<const float*>(sx.data_ptr()), static_cast<const int8_t*>(w.data_ptr()),
-                      static_cast<const float*>(sw.data_ptr()), (int)M, (int)N, (int)K, y.data_ptr(), st.stream());
+    const int rc = unlocked(fn, static_cast<const int8_t*>(x.data_ptr()), static_cast<const float*>(sx.data_ptr()), static_cast<const int8_t*>(w.data_ptr()),
+                            static_cast<const float*>(sw.data_ptr()), (int)M, (int)N, (int)K, y.data_ptr(), st.stream());
     return rc == 0 ? THPVariable_Wrap(y) : PyLong_FromLong(rc);
   } catch (const std::exception&) {
     Py_RETURN_NONE;
@@ -232,8 +242,8 @@ PyObject* kv8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const razer_kv8* c = cache.get(a[1], a[2], dev);
     const at::Tensor &k = tensor(a[3]), &v = tensor(a[4]);
     if (!c || !rows(k, c->heads, c->head_dim, dev) || !rows(v, c->heads, c->head_dim, dev) || k.size(0) != v.size(0) || !batch(a + 5, dev)) Py_RETURN_NONE;
-    return PyLong_FromLong(fn(c, k.data_ptr(), stride_of(k), v.data_ptr(), stride_of(v), ints(a[5]), (int)tensor(a[5]).size(1), ints(a[6]), ints(a[7]),
-                              (int)tensor(a[7]).size(0), (int)k.size(0), st.stream()));
+    return PyLong_FromLong(unlocked(fn, c, k.data_ptr(), stride_of(k), v.data_ptr(), stride_of(v), ints(a[5]), (int)tensor(a[5]).size(1), ints(a[6]), ints(a[7]),
+                                    (int)tensor(a[7]).size(0), (int)k.size(0), st.stream()));
   } catch (const std::exception&) {
     Py_RETURN_NONE;
   }
@@ -259,8 +269,8 @@ PyObject* attn_kv8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !whole(lse, at::kFloat, dev, {T, H}))
       Py_RETURN_NONE;
     const float scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : (float)PyFloat_AS_DOUBLE(a[7]);
-    const int rc = fn(c, q.data_ptr(), stride_of(q), (int)H, ints(a[4]), (int)tensor(a[4]).size(1), ints(a[5]), ints(a[6]), (int)tensor(a[6]).size(0), (int)T, scale,
-                      out.data_ptr(), static_cast<float*>(lse.data_ptr()), ws.data_ptr(), (size_t)ws.numel(), st.stream());
+    const int rc = unlocked(fn, c, q.data_ptr(), stride_of(q), (int)H, ints(a[4]), (int)tensor(a[4]).size(1), ints(a[5]), ints(a[6]), (int)tensor(a[6]).size(0), (int)T, scale,
+                            out.data_ptr(), static_cast<float*>(lse.data_ptr()), ws.data_ptr(), (size_t)ws.numel(), st.stream());
     return rc == 0 ? pair_of(out, lse) : PyLong_FromLong(rc);
   } catch (const std::exception&) {
     Py_RETURN_NONE;

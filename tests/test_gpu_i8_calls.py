@@ -1,0 +1,26 @@
+"""The 8-bit operators' calls: what they refuse, what they leave alone, and what they let others do."""
+import ctypes
+
+import pytest
+import torch
+
+from test_gpu_kv8 import Batch, b, fresh, queries  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_compiled_calls_let_other_threads_run(b):  # noqa: F811
+    """The library's function is called without the interpreter's lock, as through ctypes: PyGILState_Check in its place says whether the thread holds it, 0 or 1,
+    which the call takes for the library's status."""
+    if b._call is None:
+        pytest.skip(b.call_route())
+    check = ctypes.cast(ctypes.pythonapi.PyGILState_Check, ctypes.c_void_p).value
+    s = Batch([1], [40], 2, 64, 16, seed=52).device(b)
+    q, (k, v) = queries(s, 4).cuda(), (x.cuda() for x in fresh(s))
+    ws = b.alloc_attn_workspace(s.cache, 8, "cuda")
+    x = torch.zeros((3, 64), dtype=torch.bfloat16, device="cuda")
+    codes, scales = b.razer_quant_i8(x)
+    assert type(b._call.quant_i8(check, x, None, None)) is tuple
+    assert torch.is_tensor(b._call.gemm_i8(check, codes, scales, codes, scales, None))
+    assert b._call.kv8_append(check, b.RazerKv8, s.cache, k, v, *s.args) == 0
+    assert type(b._call.attn_kv8(check, b.RazerKv8, s.cache, q, *s.args, None, None, None, ws)) is tuple
