@@ -481,6 +481,7 @@ def razer_attn_kv8(cache: RazerKv8, q: torch.Tensor, block_table: torch.Tensor, 
     if workspace is None:
         workspace = alloc_attn_workspace(cache, q_heads, q.device)
     assert out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (T, q_heads)
+    assert workspace.dtype == torch.uint8 and workspace.is_contiguous()        # its elements are counted as bytes
     assert lse.is_contiguous() and _here(cache.tensors[0], q, block_table, q_start, kv_len, out, lse, workspace)
     _check(_lib.razer_attn_kv8(ctypes.byref(cache), _ptr(q), q_stride, q_heads, _ptr(block_table), block_table.shape[1], _ptr(q_start), _ptr(kv_len), B, T,
                                cache.head_dim ** -0.5 if scale is None else float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),

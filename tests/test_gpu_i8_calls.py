@@ -24,3 +24,13 @@ def test_compiled_calls_let_other_threads_run(b):  # noqa: F811
     assert torch.is_tensor(b._call.gemm_i8(check, codes, scales, codes, scales, None))
     assert b._call.kv8_append(check, b.RazerKv8, s.cache, k, v, *s.args) == 0
     assert type(b._call.attn_kv8(check, b.RazerKv8, s.cache, q, *s.args, None, None, None, ws)) is tuple
+
+
+def test_workspaces_that_are_no_bytes_side_by_side(b):  # noqa: F811
+    """A workspace whose numbers are not bytes side by side is not taken for one.  (All of these have the memory behind them.)"""
+    s = Batch([1], [40], 2, 64, 16, seed=51).device(b)
+    q = queries(s, 4).cuda()
+    ws = b.alloc_attn_workspace(s.cache, 8, "cuda")
+    for bad in (ws[:1].expand(ws.numel()), torch.empty(2 * ws.numel(), dtype=torch.uint8, device="cuda")[::2], ws.view(torch.int32)):
+        with pytest.raises(AssertionError):
+            b.razer_attn_kv8(s.cache, q, *s.args, workspace=bad)
