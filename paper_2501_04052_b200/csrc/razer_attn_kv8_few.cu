@@ -207,8 +207,8 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
       auto ask = [&]() {
         ks_next = vs_next = __uint_as_float(0x7FC00000u);
         if (value && id_next >= 0) {
-          ks_next = __ldg(a.c.k_scales + (long long)id_next * a.c.heads + g.h);
-          vs_next = __ldg(a.c.v_scales + (long long)id_next * a.c.heads + g.h);
+          ks_next = a.c.k_scales[(long long)id_next * a.c.heads + g.h];
+          vs_next = a.c.v_scales[(long long)id_next * a.c.heads + g.h];
         }
       };
       auto step = [&]() {

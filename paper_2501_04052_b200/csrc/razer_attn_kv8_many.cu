@@ -237,8 +237,8 @@ __global__ void __launch_bounds__(448, 1) attn_kv8_many_kernel(const __grid_cons
           id_next = page_of(have + 32 + lane);
           float vs = ks = __uint_as_float(0x7FC00000u);
           if (id >= 0) {
-            ks = __ldg(a.c.k_scales + (long long)id * a.c.heads + g.h);
-            vs = __ldg(a.c.v_scales + (long long)id * a.c.heads + g.h);
+            ks = a.c.k_scales[(long long)id * a.c.heads + g.h];
+            vs = a.c.v_scales[(long long)id * a.c.heads + g.h];
           }
           lg = vs >= 0.0f && vs < INFINITY ? log2f(vs) : __uint_as_float(0x7FC00000u);   // -infinity for 0
           if (ks < 0.0f) ks = __uint_as_float(0x7FC00000u);

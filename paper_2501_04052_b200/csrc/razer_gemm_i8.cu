@@ -99,14 +99,14 @@ __device__ __forceinline__ void add_parts(const I8Args& a, uint32_t part, int n_
   const bool wide = n + 4 <= a.N && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 7) == 0;
   float sw[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) sw[i] = n + i < a.N ? __ldg(a.sw + n + i) : 0.0f;
+  for (int i = 0; i < 4; ++i) sw[i] = n + i < a.N ? a.sw[n + i] : 0.0f;
   for (int m0 = t / quads; m0 < valid; m0 += 4 * step) {
     int4 sum[4];
     float sx[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       sum[u] = make_int4(0, 0, 0, 0);
-      sx[u] = m0 + u * step < valid ? __ldg(a.sx + m_tile + m0 + u * step) : 0.0f;
+      sx[u] = m0 + u * step < valid ? a.sx[m_tile + m0 + u * step] : 0.0f;
     }
     for (int p = 0; p < split; p += 2) {
       int4 v[2][4];
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(192, CTAS) i8_split_kernel(const __grid_consta
   const int row = 32 * (warp & 3) + lane;
   if (split == 1) {
     if (warp >= 2) {
-      for (int i = threadIdx.x - 64; i < NT; i += 128) scales[i] = tt * NT + i < a.M ? __ldg(a.sx + tt * NT + i) : 0.0f;
+      for (int i = threadIdx.x - 64; i < NT; i += 128) scales[i] = tt * NT + i < a.M ? a.sx[tt * NT + i] : 0.0f;
       threads_meet<128>();
       if (!mbar_wait(bar_acc, 0, words + 2)) *abort_flag = 1;
       __syncwarp();
@@ -411,8 +411,8 @@ __global__ void __launch_bounds__(320, 1) i8_pair_kernel(const __grid_constant__
       const int rt = tile / a.token_tiles, tt = tile - rt * a.token_tiles, acc = turn & 1;
       const int n = rt * 256 + rank * 128 + row, m0 = tt * NT, valid = min(NT, a.M - m0);
       float* sx = scales + acc * NT;                        // of two, so that one meeting a tile is enough
-      for (int i = threadIdx.x - 64; i < NT; i += 256) sx[i] = m0 + i < a.M ? __ldg(a.sx + m0 + i) : 0.0f;
-      const float sw = n < a.N ? __ldg(a.sw + n) : 0.0f;
+      for (int i = threadIdx.x - 64; i < NT; i += 256) sx[i] = m0 + i < a.M ? a.sx[m0 + i] : 0.0f;
+      const float sw = n < a.N ? a.sw[n] : 0.0f;
       threads_meet<256>();
       if (!mbar_wait(bar_accfull + 8 * acc, (uint32_t)(turn >> 1 & 1), abort_flag)) *abort_flag = 1;
       const bool bad = __any_sync(0xFFFFFFFFu, *abort_flag != 0);

@@ -30,8 +30,8 @@ struct Kv8Seq {
 __device__ __forceinline__ bool kv8_over(const Kv8& c, const Kv8Batch& s, int len) { return len > s.width << c.page_log2; }
 __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Batch& s, int b) {
   Kv8Seq q;
-  const int lo = __ldg(s.q_start + b), hi = __ldg(s.q_start + b + 1);
-  q.len = max(__ldg(s.kv_len + b), 0);
+  const int lo = s.q_start[b], hi = s.q_start[b + 1];
+  q.len = max(s.kv_len[b], 0);
   const bool good = lo >= 0 && hi <= s.T && hi >= lo;
   q.row0 = good ? lo : 0;
   q.n = good ? hi - lo : 0;
@@ -41,7 +41,7 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Batch& s, int b) {
 // The page of block c of sequence b, or -1 where the table is too narrow for it or names no page.
 __device__ __forceinline__ int kv8_page(const Kv8& c, const Kv8Batch& s, int b, int block) {
   if (block >= s.width) return -1;
-  const int p = __ldg(s.table + (long long)b * s.width + block);
+  const int p = s.table[(long long)b * s.width + block];
   return p >= 0 && p < c.pages ? p : -1;
 }
 

@@ -21,7 +21,7 @@ constexpr int append_threads(int D, int page) { return D * page >= 8192 ? 256 : 
 
 template <int D, int PAGE>
 __global__ void __launch_bounds__(append_threads(D, PAGE)) kv8_append_kernel(const __grid_constant__ Kv8 c, const __grid_constant__ Kv8Batch s,
-                                                                             const __nv_bfloat16* __restrict__ k_new, const __nv_bfloat16* __restrict__ v_new,
+                                                                             const __nv_bfloat16* k_new, const __nv_bfloat16* v_new,
                                                                              long long k_stride, long long v_stride) {
   constexpr int THREADS = append_threads(D, PAGE), VECS = D / 8, VPT = (PAGE * VECS + THREADS - 1) / THREADS;   // vectors of 8 values, of a row and of a thread
   constexpr int LOG2 = PAGE == 16 ? 4 : PAGE == 32 ? 5 : PAGE == 64 ? 6 : 7;
@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(append_threads(D, PAGE)) kv8_append_kernel(con
   int before = 0;                                            // sequences whose slots begin at or before this one
   for (int b0 = 0; b0 < s.B; b0 += THREADS) {
     const int b = b0 + tid;
-    const bool here = b < s.B && (long long)(max(__ldg(s.q_start + b), 0) >> LOG2) + 2LL * b <= slot;
+    const bool here = b < s.B && (long long)(max(s.q_start[b], 0) >> LOG2) + 2LL * b <= slot;
     before += __syncthreads_count(here);
   }
   if (before == 0) return;

@@ -101,7 +101,8 @@ __device__ __forceinline__ bool elect_one() {
 // Programmatic dependent launch: when the kernel was launched with the programmatic-serialization
 // attribute, `grid_dep_wait` returns once the preceding kernel in the stream has completed (otherwise at
 // once); everything that may depend on that kernel (activations, workspace, outputs) is touched after it,
-// while the weight stream, which depends on nothing, starts before.
+// while the weight stream, which depends on nothing, starts before.  What that kernel may have written is read by ordinary loads: those
+// that promise memory which does not change during the kernel (__ldg, const __restrict__) may go by another cache, or move above the wait.
 __device__ __forceinline__ void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -37,8 +37,8 @@ __device__ __forceinline__ void vec_store(uint4 v, const I8Step& t, int8_t* row,
 
 // ROWS rows a CTA, WARPS warps a row.  HELD: the row fits the threads' registers.
 template <bool FP32, int WARPS, int ROWS, int VPT, bool HELD>
-__global__ void __launch_bounds__(32 * WARPS * ROWS) quant_i8_kernel(const uint4* __restrict__ x, int M, int vecs, long long row_vecs,
-                                                                     int8_t* __restrict__ codes, float* __restrict__ scales) {
+__global__ void __launch_bounds__(32 * WARPS * ROWS) quant_i8_kernel(const uint4* x, int M, int vecs, long long row_vecs,
+                                                                     int8_t* codes, float* scales) {
   constexpr int TPR = 32 * WARPS;
   __shared__ uint32_t tops[WARPS > 1 ? WARPS * ROWS : 1];
   const int at = threadIdx.x % TPR, r = threadIdx.x / TPR;

@@ -34,3 +34,32 @@ def test_workspaces_that_are_no_bytes_side_by_side(b):  # noqa: F811
     for bad in (ws[:1].expand(ws.numel()), torch.empty(2 * ws.numel(), dtype=torch.uint8, device="cuda")[::2], ws.view(torch.int32)):
         with pytest.raises(AssertionError):
             b.razer_attn_kv8(s.cache, q, *s.args, workspace=bad)
+
+
+@pytest.mark.parametrize("H,D,page,B,G", [(8, 128, 16, 70, 4), (8, 64, 128, 40, 1), (2, 64, 16, 150, 1), (4, 128, 32, 5, 40)])
+def test_scales_that_the_kernel_directly_ahead_has_written(b, H, D, page, B, G):  # noqa: F811
+    """The writer raises the scales of pages, several to a cache line and each by a CTA that has read the line before, and the attention behind it is resident by then: as if
+    every call had been waited for."""
+    steps, width = 25, 3
+    g = torch.Generator().manual_seed(B)
+    table = torch.randperm(B * width, generator=g).view(B, width).int().cuda()
+    starts = torch.arange(B + 1, dtype=torch.int32).cuda()
+    lens = torch.randint(page + 1, 2 * page, (B,), generator=g, dtype=torch.int32).cuda()
+    news = [[(torch.randn((B, H, D), generator=g) * 1.05 ** i).bfloat16().cuda() for _ in range(2)] for i in range(steps)]
+    q = torch.randn((B, H * G, D), generator=g).bfloat16().cuda()
+    pool = torch.randint(-127, 128, (B * width, H, page, D), generator=g, dtype=torch.int8).cuda()
+    want = None
+    for wait in (True, False, False, False):
+        cache = b.make_kv8(pool.clone(), pool.clone(), *(torch.full((B * width, H), 1e-3, device="cuda") for _ in range(2)))
+        ws = b.alloc_attn_workspace(cache, H * G, "cuda")
+        got = []
+        for k, v in news:
+            b.razer_kv8_append(cache, k, v, table, starts, lens)
+            if wait:
+                torch.cuda.synchronize()
+            got.append(b.razer_attn_kv8(cache, q, table, starts, lens, workspace=ws))
+            if wait:
+                torch.cuda.synchronize()
+        b.razer_workspace_status(ws)
+        want = want or got
+        assert all(torch.equal(x, y) for a, c in zip(got, want) for x, y in zip(a, c))
