@@ -1,10 +1,11 @@
 """The 8-bit operators' calls: what they refuse, what they leave alone, and what they let others do."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_kv8 import Batch, b, fresh, queries  # noqa: F401
+from test_gpu_kv8 import Batch, append64, b, fresh, queries  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,45 @@ def test_scales_that_the_kernel_directly_ahead_has_written(b, H, D, page, B, G):
         b.razer_workspace_status(ws)
         want = want or got
         assert all(torch.equal(x, y) for a, c in zip(got, want) for x, y in zip(a, c))
+
+
+def test_append_leaves_what_bad_rows_would_write(b):  # noqa: F811
+    """q_start that leaves 0 .. T: those sequences write nothing, the others all of theirs."""
+    for starts, bad in (([0, 2, 5, 9], [2]), ([-1, 2, 5, 7], [0]), ([-3, -1, 4, 8], [0, 1, 2])):
+        s = Batch([2, 3, 2], [20, 30, 40], 2, 64, 16, seed=63)
+        k, v = fresh(s)
+        s.starts = np.array(starts, dtype=np.int32)
+        s.device(b)
+        b.razer_kv8_append(s.cache, k.cuda(), v.cuda(), *s.args)
+        s.new = [0 if i in bad else starts[i + 1] - starts[i] for i in range(3)]
+        for x, codes, scales, got_c, got_s in ((k, s.k, s.ks, s.dev[0], s.dev[2]), (v, s.v, s.vs, s.dev[1], s.dev[3])):
+            want_c, want_s = append64(s, x, codes, scales)
+            assert np.array_equal(got_c.cpu().numpy(), want_c) and np.array_equal(got_s.cpu().numpy(), want_s), starts
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_attention_refuses_bad_tensors_beside_a_workspace(b, monkeypatch, compiled):  # noqa: F811
+    """A call with a workspace of its own goes through the compiled part first."""
+    if compiled and b._call is None:
+        pytest.skip(b.call_route())
+    if not compiled:
+        monkeypatch.setattr(b, "_call", None)
+    s = Batch([3, 1], [40, 90], 2, 64, 16, seed=50).device(b)
+    q = queries(s, 4).cuda()
+    ws = b.alloc_attn_workspace(s.cache, 8, "cuda")
+    table, starts, lens = s.args
+    out, lse = torch.empty_like(q), torch.empty((s.T, 8), device="cuda")
+    for bad in (q.float(), q[:, :, ::2], q.transpose(0, 1), q.cpu(), q[0]):
+        with pytest.raises((AssertionError, RuntimeError, IndexError)):
+            b.razer_attn_kv8(s.cache, bad, *s.args, workspace=ws)
+    for args in ((table.long(), starts, lens), (table.t(), starts, lens), (table[:1], starts, lens), (table, starts[:2], lens), (table, starts, lens[:1]), (table, starts.cpu(), lens)):
+        with pytest.raises((AssertionError, RuntimeError)):
+            b.razer_attn_kv8(s.cache, q, *args, workspace=ws)
+    for other in (dict(out=out.float()), dict(out=out[:2]), dict(out=out.transpose(0, 1)), dict(lse=lse.double()), dict(lse=lse[:, :4]), dict(out=out.cpu())):
+        with pytest.raises((AssertionError, RuntimeError)):
+            b.razer_attn_kv8(s.cache, q, *s.args, workspace=ws, **other)
+    with pytest.raises(b.RazerError):
+        b.razer_attn_kv8(s.cache, q, *s.args, workspace=ws, scale=float("nan"))
+    want = b.razer_attn_kv8(s.cache, q, *s.args)
+    got = b.razer_attn_kv8(s.cache, q, *s.args, workspace=ws, out=out, lse=lse)
+    assert got[0].data_ptr() == out.data_ptr() and torch.equal(out, want[0]) and torch.equal(lse, want[1])
