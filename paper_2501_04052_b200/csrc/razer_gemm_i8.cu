@@ -90,10 +90,10 @@ struct I8Args {
   int token_tiles, chunks;     // chunks: stages of the whole K
 };
 
-// The sums of a cluster's CTAs over K, [token][128 rows] at `part` of each: CTA `mine` of the `split` (ranks `stride` apart from `first`) adds up and
+// The sums of a cluster's CTAs over K, [token][128 rows] at `part` of each: CTA `mine` of the `split` adds up and
 // stores 128 / split of the rows, four rows a thread (16 bytes of sums, 8 of results), four tokens in flight.
 template <int THREADS>
-__device__ __forceinline__ void add_parts(const I8Args& a, uint32_t part, int n_tile, int m_tile, int valid, int split, int mine, int stride, int first, int t, bool bad) {
+__device__ __forceinline__ void add_parts(const I8Args& a, uint32_t part, int n_tile, int m_tile, int valid, int split, int mine, int t, bool bad) {
   const int quads = TILE_ROWS / 4 / split, r = 4 * (mine * quads + t % quads), n = n_tile + r, step = THREADS / quads;
   if (n >= a.N) return;
   const bool wide = n + 4 <= a.N && a.N % 4 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 7) == 0;
@@ -113,7 +113,7 @@ __device__ __forceinline__ void add_parts(const I8Args& a, uint32_t part, int n_
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[h][u] = peer_lds128(part + (uint32_t)(min(m0 + u * step, valid - 1) * TILE_ROWS + r) * 4, first + (p + h) * stride);
+        for (int u = 0; u < 4; ++u) v[h][u] = peer_lds128(part + (uint32_t)(min(m0 + u * step, valid - 1) * TILE_ROWS + r) * 4, p + h);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -165,6 +165,7 @@ __global__ void __launch_bounds__(192, CTAS) i8_split_kernel(const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = split > 1 ? (int)cluster_rank() : 0;
   const int tile = blockIdx.x / split, rt = tile / a.token_tiles, tt = tile - rt * a.token_tiles;
+  // never empty: K is split only where every part has two stages
   const int c_begin = (int)((long long)a.chunks * rank / split), c_end = (int)((long long)a.chunks * (rank + 1) / split);
 
   if (threadIdx.x == 0) {
@@ -224,7 +225,6 @@ __global__ void __launch_bounds__(192, CTAS) i8_split_kernel(const __grid_consta
     mbar_wait(bar_acc, 0, words + 2);
     __syncwarp();
   }
-  const bool any = c_end > c_begin;
   float* scales = reinterpret_cast<float*>(i8_smem + (bars + 256 - smem_u32(i8_smem)));
   const int row = 32 * (warp & 3) + lane;
   if (split == 1) {
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(192, CTAS) i8_split_kernel(const __grid_consta
         tc_wait_ld();
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + (uint32_t)((c + j) * TILE_ROWS + row) * 4), "r"(any ? v[j] : 0u) : "memory");
+          asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + (uint32_t)((c + j) * TILE_ROWS + row) * 4), "r"(v[j]) : "memory");
       }
       tc_fence_before();
     }
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(192, CTAS) i8_split_kernel(const __grid_consta
     if (warp >= 2) {
       bool bad = false;
       for (int p = 0; p < split; ++p) bad |= peer_lds32(smem_u32(words + 1), p) != 0;
-      add_parts<128>(a, base, rt * TILE_ROWS, tt * NT, min(NT, a.M - tt * NT), split, rank, 1, 0, threadIdx.x - 64, bad);
+      add_parts<128>(a, base, rt * TILE_ROWS, tt * NT, min(NT, a.M - tt * NT), split, rank, threadIdx.x - 64, bad);
     }
     __syncwarp();
     cluster_meet();                                         // nobody leaves while another reads its sums
