@@ -314,7 +314,7 @@ int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_
  * the cache's heads, query head i reads key-value head i / (q_heads / heads).  The row of a token at position p = kv_len - n + i sees
  * the keys 0 .. p:
  *   s_j = scale * k_scale(page of j) * <q, k_code_j>,  out = sum_j exp(s_j) v_scale(page of j) v_code_j / sum_j exp(s_j)
- * out_dev: bf16 [T][q_heads][head_dim], 16-byte aligned; lse_dev: FP32 [T][q_heads], log sum_j exp(s_j), or NULL.  A row that
+ * scale: at most 2^62 in magnitude.  out_dev: bf16 [T][q_heads][head_dim], 16-byte aligned; lse_dev: FP32 [T][q_heads], log sum_j exp(s_j), or NULL.  A row that
  * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN or negative shows as NaN in the rows that see its
  * page, and so do a page that the table does not name and a NaN or an infinity among a row's queries; a sequence longer than the table
  * gets NaN in all its rows.  Keys and values count exactly, sums are FP32.  What is rounded follows the kernel, and that the mean of the

@@ -532,7 +532,8 @@ int razer_attn_kv8(const razer_kv8* cache, const void* q_dev, long long q_stride
   RAZER_TRY(check_kv8(cache, c));
   RAZER_TRY(check_heads(c, q_heads));
   RAZER_TRY(check_batch(cache, block_table_dev, table_width, q_start_dev, kv_len_dev, B, T, s));
-  if (!std::isfinite(scale)) return set_error(RAZER_ERR_INVALID_ARG, "scale %g is not finite", scale);
+  // times log2 e and a row's power of two (2^63 at most, queries being bf16) it has to stay finite: infinity times a score of 0 would be NaN
+  if (!(std::fabs(scale) <= 0x1p62f)) return set_error(RAZER_ERR_INVALID_ARG, "scale %g is not finite, or beyond 2^62", scale);
   if (B == 0 || T == 0) return RAZER_OK;
   RAZER_TRY(check_rows(q_dev, q_stride, (long long)q_heads * c.D, "q_dev"));
   RAZER_TRY(check_ptr(out_dev, 16, "out_dev"));

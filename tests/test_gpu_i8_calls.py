@@ -106,3 +106,32 @@ def test_attention_refuses_bad_tensors_beside_a_workspace(b, monkeypatch, compil
     want = b.razer_attn_kv8(s.cache, q, *s.args)
     got = b.razer_attn_kv8(s.cache, q, *s.args, workspace=ws, out=out, lse=lse)
     assert got[0].data_ptr() == out.data_ptr() and torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("new,total,G", [([1, 1], [300, 40], 4), ([1], [3000], 8), ([70], [200], 4), ([300], [900], 4)])
+def test_attention_without_a_log_sum(b, new, total, G):  # noqa: F811
+    """lse_dev NULL: the same output, by either kernel, from whole units and from joined parts."""
+    s = Batch(new, total, 2, 128, 32, seed=53).device(b)
+    q = queries(s, G).cuda()
+    ws = b.alloc_attn_workspace(s.cache, 2 * G, "cuda")
+    want, _ = b.razer_attn_kv8(s.cache, q, *s.args, workspace=ws)
+    out = torch.empty_like(q)
+    table, starts, lens = s.args
+    rc = b.lib().razer_attn_kv8(ctypes.byref(s.cache), q.data_ptr(), q.stride(0), 2 * G, table.data_ptr(), table.shape[1], starts.data_ptr(), lens.data_ptr(), len(new), s.T,
+                                128 ** -0.5, out.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    b.razer_workspace_status(ws)
+    assert torch.equal(out, want)
+
+
+def test_attention_with_the_largest_scale(b):  # noqa: F811
+    """Scores of 0 under it are 0, by either kernel."""
+    for rows in (1, 40):
+        s = Batch([1], [200], 1, 64, 16, seed=54)
+        s.k[:] = 0
+        q = queries(s, rows)
+        s.device(b)
+        for scale in (2.0 ** 62, -2.0 ** 62):
+            out, lse = b.razer_attn_kv8(s.cache, q.cuda(), *s.args, scale=scale)
+            plain, plain_lse = b.razer_attn_kv8(s.cache, q.cuda(), *s.args, scale=0.0)
+            assert torch.equal(out, plain) and torch.equal(lse, plain_lse)
