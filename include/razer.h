@@ -301,7 +301,7 @@ typedef struct razer_kv8 {
  * tokens, with s0 the scale so far (0 where the page's first token is new) and a the largest new magnitude: the scale becomes
  * s = max(s0, fl32(a / 127)) (2^-149 as in razer_quant_i8); where s > s0 > 0 the page's other codes become the nearest integers to
  * the exact code * s0 / s, so that they keep their values; the new codes are the nearest integers to the exact x / s.  A NaN or an infinity among
- * the new values, or s0 NaN, makes the page's scale NaN for that head (new codes 0, the others as they were).  Tokens whose
+ * the new values, or s0 NaN or infinite, makes the page's scale NaN for that head (new codes 0, the others as they were).  Tokens whose
  * page the table does not name (an entry outside 0 .. pages - 1, or behind table_width) or whose position is negative (more new
  * tokens than kv_len) are not written.  A page that gets tokens belongs to one sequence and one place of its table; pages that
  * sequences share must be full ones. */
@@ -318,7 +318,8 @@ int razer_kv8_append(const razer_kv8* cache, const void* k_new_dev, long long k_
  * sees no key (p < 0, kv_len 0) gets zeros and lse = -infinity.  A scale that is NaN or negative shows as NaN in the rows that see its
  * page, and so do a page that the table does not name and a NaN or an infinity among a row's queries; a sequence longer than the table
  * gets NaN in all its rows.  Keys and values count exactly, sums are FP32.  What is rounded follows the kernel, and that the mean of the
- * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head.  Up to 32 rows: queries to 2^-22 of their row's largest
+ * batch, (T / B) * (q_heads / heads) rows for each sequence and key-value head (so that a sequence's last bits may change with its
+ * neighbours).  Up to 32 rows: queries to 2^-22 of their row's largest
  * magnitude (24-bit fixed point: bf16 exactly down to 2^-14 of it), weights exp(s_j) v_scale to 2^-25 of the largest that the
  * row sees among 128 consecutive keys.  More: both to f16, queries relative to their row's largest magnitude (bf16 exactly down to 2^-28 of it), weights
  * with 11 significant bits or to 2^-30 of the row's largest exp(s_j) times the largest value scale among the pages that it sees.

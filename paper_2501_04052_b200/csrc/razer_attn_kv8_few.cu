@@ -16,10 +16,11 @@
 // through shared memory), exponentials, digits to shared memory, and O = O f + O_tile in FP32 registers.  Work is cut evenly
 // among the CTAs as razer_attn_kv8.cuh says.
 //
-// What bounds it: instructions, then HBM.  64 sequences of up to 16384 tokens, 8 x 8 heads of 128 (1.28 GB) 201 to 214 us (6.0 to 6.4 TB/s) as long as the clock is up; in
+// What bounds it: the chain of a tile in each softmax group (scores, maxima, the group's meeting, exponentials, digits; every instruction in it counts, while issue slots are 37 %
+// busy and HBM 56 % at 8 rows and 26 % at 32), then HBM.  64 sequences of up to 16384 tokens, 8 x 8 heads of 128 (1.28 GB) 201 to 214 us (6.0 to 6.4 TB/s) as long as the clock is up; in
 // a loop of some seconds the GPU is at its power limit (1000 W, 1700 instead of 1965 MHz) and the call takes 228 (241 before rows went two to an instruction, packed
-// FP32, and maxima by redux.sync).  32 sequences of 4096 tokens: 54 us for 8 rows, 76 for 16, 121 for 32 (83 and 169 before that).  One sequence of 4096 tokens, 8 x 4 heads
-// of 64: 11.6, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  Heads of 64: 79 us for 268 MB in pages of 64, 95 in pages
+// FP32, and maxima by redux.sync).  32 sequences of 4096 tokens: 54 us for 8 rows, 77 for 16, 122 for 32 (83 and 169 before that).  One sequence of 4096 tokens, 8 x 4 heads
+// of 64: 11.4 a call, 11.6 in a graph, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  Heads of 64: 80 us for 268 MB in pages of 64, 95 in pages
 // of 16 (boxes of 1 KB).
 #include "razer_attn_kv8.cuh"
 
@@ -672,7 +673,7 @@ int launch_as(AttnArgs& a, cudaStream_t st) {
 size_t attn_few_part_floats(int D) { return D == 64 ? FewCfg<64, 32>::PART_FLOATS : FewCfg<128, 32>::PART_FLOATS; }
 
 int launch_attn_few(AttnArgs& a, int rows, cudaStream_t st) {
-  // Four rows at most (64 sequences of 4096 tokens, 8 x 4 heads): half of eight's work, heads of 64 79 us against 88, of 128 (32 sequences) 55 against 57.
+  // Four rows at most (64 sequences of 4096 tokens, 8 x 4 heads): half of eight's work, heads of 64 80 us against 88, of 128 (32 sequences) 55 against 57.
   if (rows <= 4) return a.c.D == 64 ? launch_as<64, 8, 4>(a, st) : launch_as<128, 8, 4>(a, st);
   if (a.c.D == 64) return rows <= 8 ? launch_as<64, 8>(a, st) : rows <= 16 ? launch_as<64, 16>(a, st) : launch_as<64, 32>(a, st);
   return rows <= 8 ? launch_as<128, 8>(a, st) : rows <= 16 ? launch_as<128, 16>(a, st) : launch_as<128, 32>(a, st);

@@ -10,12 +10,14 @@
 // first tiles next to never.  Queries are f16 with a power of two of their row's own (largest magnitude in [2^14, 2^15)), probabilities f16
 // times 2^6 (11 significant bits, at most 2^14 before the maximum follows, down to 2^-30); value scales enter the probabilities relative to
 // twice the largest that the row has met.  (Of the pages that it sees: one for all rows of a tile would leave a row whose own pages have values 2^33 times
-// smaller than those behind its mask without any weight.)
+// smaller than those behind its mask without any weight.)  Probabilities in f16 are what the MMA takes beside f16 codes; their roundings are independent and an eighth of that
+// of a bf16 output: against 64 bits the chunk below is off by 0.00167 of its norm, by FP32 probabilities by 0.00166, the two apart by 0.00087 where one of them rounds the other
+// way.  The sums of the exponentials are FP32 of what was not rounded.
 // A pair of CTAs (cta_group::2) takes 512 rows: each converts half of the keys of a step and half of the values' dimensions, so that a tile is
 // converted once for both, and the MMAs read half as much of it from either's shared memory.
-// What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 352 us (751 TFLOP/s) by pairs, 373 without: 2300 to 2500 cycles
+// What bounds it: 3 ragged sequences of up to 8192 tokens, up to 1000 of them new, 8 x 4 heads of 128, 355 us (746 TFLOP/s) by pairs, 373 without: 2300 to 2500 cycles
 // for 256 rows x 64 tokens.  Without the softmax a single CTA takes 2200 (the MMAs of S, half as wide as they are long, 860, those of O 300, and shared memory that these share
-// with the conversion, 48 KB), a pair 1600.  The exponentials alone are 1024 (16 a cycle); XU 39 %, ALU 36 %, tensor 35 % busy, issue slots 47 %: what is left is
+// with the conversion, 48 KB), a pair 1600.  The exponentials alone are 1024 (16 a cycle); By pairs XU 43 %, ALU 37 %, tensor 39 % busy, issue slots 49 %: what is left is
 // the chain of a step (scores read, maximum, exponentials, probabilities stored, 1900 cycles), of which a scheduler has two to interleave.
 // A unit's ends (queries in, sums out, parts joined) are a tenth of the time.
 // Row tiles of a sequence are taken in the order first, last, second, last but one ..., so that equal runs of them are about equal work under the

@@ -7,7 +7,8 @@
 // tiles than SMs, and every weight byte comes from HBM once whatever the split.  The parts meet in distributed shared memory - integers, so that their
 // order does not matter - and each CTA finishes 128 / split of the rows: no workspace, no counters, nothing left between calls.
 //
-// i8_pair_kernel: two CTAs on 256 weight rows x up to 256 tokens, for more tokens than a few dozen (below).
+// i8_pair_kernel: two CTAs on 256 weight rows x up to 256 tokens, where the cost model below finds it faster (from 33 tokens on; narrow products of some hundred tokens
+// stay with the other).
 //
 // What bounds them, in a graph (a host loop in brackets, where the power limit lowers the clock): 1 x 11008 x 4096 10.2 us (11.0), 16 x 28672 x 8192 38.8 (40.1,
 // 5.9 TB/s): the weights from HBM, and the launch; 333 x 4096 x 11008 17 (21): 64 pairs of CTAs that take in 1.9 MB a CTA at 150 GB/s;

@@ -6,7 +6,7 @@
 // codes, and a code that moves to the new scale does so by a table of 256.  Which page a CTA has follows from q_start alone: sequence b has the
 // slots from q_start[b] / page + 2 b on, which is room enough (n tokens touch at most n / page + 2 pages), so that the grid T / page + 2 B needs
 // nothing from the device.  What bounds it: latency for a decode step (a chain of five loads: 64 tokens x 8 heads 3.7 us
-// a call), for prompts the same chain in three rounds of CTAs and the bytes (46 MB 13.4 us, 3.4 TB/s).
+// a call), for prompts the same chain in three rounds of CTAs and the bytes (46 MB 13.4 us in a graph, 3.4 TB/s, 14.7 a call from the host).
 #include "razer_common.cuh"
 #include "razer_i8.cuh"
 #include "razer_kv8.cuh"
@@ -16,7 +16,7 @@ namespace razer {
 
 namespace {
 
-// 14.3 M values in pages of 64 x 128: 128 threads 14.2 us, 256 13.4, 512 19.1
+// 14.3 M values in pages of 64 x 128, in a graph: 128 threads 14.2 us, 256 13.4, 512 19.1
 constexpr int append_threads(int D, int page) { return D * page >= 8192 ? 256 : 128; }
 
 template <int D, int PAGE>

@@ -1,8 +1,8 @@
 // Rows to 8-bit integers with a scale each: tokens online, weight channels offline (razer_quant_i8).
 //
 // One pass: a row's values stay in registers from its maximum to its codes.  WARPS warps share a row, VPT 16-byte vectors a thread;
-// the host takes the fewest warps that hold the row with VPT <= 4, so that a single token spreads over a whole CTA (latency) and the rows of a
-// large matrix still come with 16 KB a CTA in flight.  Rows too long for that (over 32 K of bf16, 16 K of FP32) are read twice, the second time
+// the host takes the fewest warps that hold the row with VPT <= 4, so that a single token spreads over a whole CTA (latency).  In flight a CTA has its rows: four of up to
+// 2 KB, or one of 2 to 64 KB (4096 FP32: 16).  Rows too long for that (over 32 K of bf16, 16 K of FP32) are read twice, the second time
 // from L2.  Bound by HBM from some MB on; the arithmetic is about 7 instructions an element (razer_i8.cuh).  11008 rows of 4096 FP32 35.4 us (6.4 TB/s),
 // 333 of 11008 bf16 4.5 (2.4 TB/s, the launch is half of it), one of 4096 1.9 in a graph; a call from the host 4.7, two allocations included.
 #include "razer_common.cuh"
