@@ -28,8 +28,8 @@ int launch_attn_kv8(const Kv8& c, const Kv8Batch& s, const void* q, long long q_
   a.scale = scale;
   a.G = q_heads / c.heads;
   // By the rows of queries that a sequence has for a key-value head, in the mean (which ones the device alone knows; either kernel takes any).  8 key-value
-  // heads x 8, 32 sequences of 4096 tokens, pages of 64, microseconds with few / many rows: 8 rows 54 / 193, 16 77 / 195, 32 122 / 199,
-  // 48 219 / 200 (the tile of 32 taken twice), 128 413 / 202.  Pairs of CTAs
+  // heads x 8, 32 sequences of 4096 tokens, pages of 64, microseconds with few / many rows: 8 rows 54 / 193, 16 78 / 196, 32 121 / 199,
+  // 48 217 / 200 (the tile of 32 taken twice), 128 408 / 202.  Pairs of CTAs
   // (heads of 128) from 1024 rows on where a row tile of 512 is at most 128 tokens, so that the causal mask wastes little of it, many rows / pairs: 3 ragged
   // sequences of 8192 with 4 x 1000 rows 373 / 355, 8192 rows over 32768 tokens 1231 / 1081, 2400 rows over 4000 87 / 83, 1024 over 8192 82 / 80; 512 over
   // 8192 70 / 72, 510 over 4096 73 / 81, 2048 tokens among themselves with one query head 109 / 119.  RAZER_ATTN (environment, read once; a test aid): "few",

@@ -7,7 +7,7 @@
 // The sums are exact in 32 bits, so that what is rounded is q to 2^-22 of its row's largest (bf16 queries exactly but for those below 2^-14
 // of it), w to 2^-25 of the tile's largest, and the FP32 arithmetic between.  One maximum serves both sums, of s + max(log2 vs, the tile's largest - 60): it
 // stays above every weight, and within 2^60 of the largest exponential.  Where value scales of a tile lie further apart (a page of zeros too) it may be far above the
-// weights that there are; their own is then found in a second round.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each
+// weights that there are; theirs is then found as well.  A tile is 128 tokens: a lane of TMEM each for S, a lane for each
 // dimension for O.  Since the digits ride along as columns (32 of S and of O for 8 rows, against 54 cycles that an MMA takes at any
 // width up to 64), they cost nothing, and a tile takes a third of the instructions that unpacking codes for mma.sync took.
 //
@@ -19,8 +19,8 @@
 // What bounds it: the chain of a tile in each softmax group (scores, maxima, the group's meeting, exponentials, digits; every instruction in it counts, while issue slots are 37 %
 // busy and HBM 56 % at 8 rows and 26 % at 32), then HBM.  64 sequences of up to 16384 tokens, 8 x 8 heads of 128 (1.28 GB) 201 to 214 us (6.0 to 6.4 TB/s) as long as the clock is up; in
 // a loop of some seconds the GPU is at its power limit (1000 W, 1700 instead of 1965 MHz) and the call takes 228 (241 before rows went two to an instruction, packed
-// FP32, and maxima by redux.sync).  32 sequences of 4096 tokens: 54 us for 8 rows, 77 for 16, 122 for 32 (83 and 169 before that).  One sequence of 4096 tokens, 8 x 4 heads
-// of 64: 11.4 a call, 11.6 in a graph, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  Heads of 64: 80 us for 268 MB in pages of 64, 95 in pages
+// FP32, and maxima by redux.sync).  32 sequences of 4096 tokens: 54 us for 8 rows, 78 for 16, 121 for 32 (83 and 169 before that).  One sequence of 4096 tokens, 8 x 4 heads
+// of 64: 11.5 a call, 11.6 in a graph, latency: launch, the look at the batch, 2 to 3 tiles a CTA, the meeting of 16 parts.  Heads of 64: 79 us for 268 MB in pages of 64, 95 in pages
 // of 16 (boxes of 1 KB).
 #include "razer_attn_kv8.cuh"
 
@@ -49,8 +49,8 @@ struct FewCfg {
   static constexpr int JOIN_BYTES = GROUPS * 32 * D > (ATTN_CTAS + 3) * R * 4 ? GROUPS * 32 * D : (ATTN_CTAS + 3) * R * 4;   // [group][8 rows][D] floats, then attn_combine's; over the digits where they have the room:
   static constexpr bool JOIN_ON_P = JOIN_BYTES <= GROUPS * P_BYTES;    // at a unit's end they have been read
   static constexpr int O_JOIN = JOIN_ON_P ? O_P : O_P + GROUPS * P_BYTES;
-  static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][2][4 warps][R]
-  static constexpr int O_STAT = O_RED + GROUPS * 8 * R * 4;            // [group][R] A, M; [group][4][R] sums
+  static constexpr int O_RED = O_P + GROUPS * P_BYTES + (JOIN_ON_P ? 0 : JOIN_BYTES);   // [group][with the floor, without][2][4 warps][R]
+  static constexpr int O_STAT = O_RED + GROUPS * 16 * R * 4;            // [group][R] A, M; [group][4][R] sums
   static constexpr int O_TABLE = O_STAT + GROUPS * 6 * R * 4;          // [warp][TABLES][8][R] what a tile means for each row
   static constexpr int O_ROW = O_TABLE + 4 * GROUPS * TABLES * R * 32; // [2][R] score factor in two parts; [2][R] keys
   static constexpr int O_META = O_ROW + 2 * R * 12;                    // [STAGES][8] {key scale, log2 of the value scale}, [STAGES] {the largest of the latter, whether they lie far apart}
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     const uint32_t t_s = tmem + lanes + group * C::S_COLS, t_o = tmem + lanes + GROUPS * C::S_COLS + group * C::P_COLS;
     const uint32_t p_at = sb + C::O_P + group * C::P_BYTES;
-    float* red = reinterpret_cast<float*>(sm + C::O_RED) + group * 8 * R;             // [2][4][R]
+    float* red = reinterpret_cast<float*>(sm + C::O_RED) + group * 16 * R;            // [2][2][4][R]
     float* stat = reinterpret_cast<float*>(sm + C::O_STAT);                           // [group][R] A, M; [group][4][R]
     float* stat_a = stat + group * R;
     float* stat_m = stat + GROUPS * R + group * R;
@@ -519,25 +519,22 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         if (lg != lg && seen) atomicOr(broken + group, seen);                         // a value scale that is none
         // The last tile's product has read its digits by then, and gives way to this one's once it is in registers: late for eight rows, here for more.
         if (CHUNKS > 1 && pending) take_all();
-        group_meet(group);
-        float common = 0.0f;                                                          // the maximum with the floor
         if (apart) {
-          // Some value scale here is so much smaller than the largest that the floor may have made the maximum, above all weights that there are: once more without it.
-          common = lane < R ? row_top(red_now) : 0.0f;
-          group_meet(group);
+          // Some value scale here is so much smaller than the largest that the floor may make the maximum, above all weights that there are: theirs as well.  (No meeting of its
+          // own: after a wait that gave up threads may have read different things here.)
           const uint64_t own = pair64(lg != lg ? -INFINITY : lg, lg != lg ? -INFINITY : lg);
 #pragma unroll
           for (int j = 0; j < R / 8 * LP; ++j) {
             const int r = j / LP * 8 + j % LP * 2;
             const uint64_t w = add2(v[r / 2], own);
             const float t0 = warp_max(low64(w)), t1 = warp_max(high64(w));
-            if (lane == 0) red_now[quarter * R + r] = t0, red_now[quarter * R + r + 1] = t1;
+            if (lane == 0) red_now[(8 + quarter) * R + r] = t0, red_now[(8 + quarter) * R + r + 1] = t1;
           }
-          group_meet(group);
         }
+        group_meet(group);
         if (lane < R) {                                                               // what all threads want to know of row `lane`
-          const float top = row_top(red_now);
-          const float mn = fmaxf(top_m, (apart ? common : top) - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
+          const float common = row_top(red_now), top = apart ? row_top(red_now + 8 * R) : common;
+          const float mn = fmaxf(top_m, common - lg_top), ms = mn == -INFINITY ? 0.0f : mn;
           const float an = fmaxf(top_a, top), as = an == -INFINITY ? 0.0f : an;
           tab[lane] = -ms;
           tab[R + lane] = top == -INFINITY ? 0.0f : -top;
@@ -673,7 +670,7 @@ int launch_as(AttnArgs& a, cudaStream_t st) {
 size_t attn_few_part_floats(int D) { return D == 64 ? FewCfg<64, 32>::PART_FLOATS : FewCfg<128, 32>::PART_FLOATS; }
 
 int launch_attn_few(AttnArgs& a, int rows, cudaStream_t st) {
-  // Four rows at most (64 sequences of 4096 tokens, 8 x 4 heads): half of eight's work, heads of 64 80 us against 88, of 128 (32 sequences) 55 against 57.
+  // Four rows at most (64 sequences of 4096 tokens, 8 x 4 heads): half of eight's work, heads of 64 79 us against 88, of 128 (32 sequences) 55 against 57.
   if (rows <= 4) return a.c.D == 64 ? launch_as<64, 8, 4>(a, st) : launch_as<128, 8, 4>(a, st);
   if (a.c.D == 64) return rows <= 8 ? launch_as<64, 8>(a, st) : rows <= 16 ? launch_as<64, 16>(a, st) : launch_as<64, 32>(a, st);
   return rows <= 8 ? launch_as<128, 8>(a, st) : rows <= 16 ? launch_as<128, 16>(a, st) : launch_as<128, 32>(a, st);
