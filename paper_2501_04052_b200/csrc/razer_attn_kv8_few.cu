@@ -478,7 +478,6 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         if (!mbar_wait(bar_vfull + 8 * stage, (uint32_t)(((item + i) / ST) & 1), abort_flag)) fail(9);
         const float2 sc = meta[stage * 8 + (tid >> a.c.page_log2)];
         const float2 most = meta_top[stage];
-        const bool apart = most.y != 0.0f;
         const float lg_top = most.x, lg = sc.y, lg_max = fmaxf(lg, lg_top - FLOOR);   // (a NaN becomes the floor)
         if (!mbar_wait(bar_sfull + 8 * group, (uint32_t)(mine & 1), abort_flag)) fail(8);
         __syncwarp();
@@ -519,9 +518,10 @@ __global__ void __launch_bounds__(FewCfg<D, R>::THREADS, 1) attn_kv8_few_kernel(
         if (lg != lg && seen) atomicOr(broken + group, seen);                         // a value scale that is none
         // The last tile's product has read its digits by then, and gives way to this one's once it is in registers: late for eight rows, here for more.
         if (CHUNKS > 1 && pending) take_all();
+        const bool apart = __any_sync(0xFFFFFFFFu, most.y != 0.0f);                   // one answer for a warp, whatever its lanes have read after a wait that gave up
         if (apart) {
           // Some value scale here is so much smaller than the largest that the floor may make the maximum, above all weights that there are: theirs as well.  (No meeting of its
-          // own: after a wait that gave up threads may have read different things here.)
+          // own: after a wait that gave up warps may have read different things here.)
           const uint64_t own = pair64(lg != lg ? -INFINITY : lg, lg != lg ? -INFINITY : lg);
 #pragma unroll
           for (int j = 0; j < R / 8 * LP; ++j) {
